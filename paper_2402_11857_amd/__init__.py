@@ -32,3 +32,10 @@ from .binding import (  # noqa: F401
     liec_step,
     liec_step_sync,
 )
+from .train import (  # noqa: F401
+    liec_clip_grads,
+    liec_gather_grads,
+    liec_grad_norm,
+    liec_layer_norm,
+    liec_layer_norm_backward,
+)

@@ -125,6 +125,21 @@ def lib():
         L.liec_status_string.argtypes = [ctypes.c_int]
         L.liec_scratch_bytes.restype = i64
         L.liec_scratch_bytes.argtypes = [vp]
+        # include/liec_train.h; the tensors' table and the structs go as addresses
+        L.liec_grads_workspace.restype = i64
+        L.liec_grads_workspace.argtypes = [i32, i32]
+        L.liec_grad_norm.restype = ctypes.c_int
+        L.liec_grad_norm.argtypes = [vp, i32, i32, vp, vp, i64, vp]
+        L.liec_clip_grads.restype = ctypes.c_int
+        L.liec_clip_grads.argtypes = [vp, i32, i32, f32, vp, vp, i64, vp]
+        L.liec_gather_grads.restype = ctypes.c_int
+        L.liec_gather_grads.argtypes = [vp, i32, i32, vp, i64, f32, vp, vp, i64, vp]
+        L.liec_layer_norm.restype = ctypes.c_int
+        L.liec_layer_norm.argtypes = [vp, vp, vp, vp, vp, vp, i32, i64, i64, f32, ctypes.c_int, ctypes.c_int, vp]
+        L.liec_layer_norm_workspace.restype = i64
+        L.liec_layer_norm_workspace.argtypes = [i32, i64, i64]
+        L.liec_layer_norm_backward.restype = ctypes.c_int
+        L.liec_layer_norm_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i64, i64, ctypes.c_int, ctypes.c_int, vp, i64, vp]
         L.liec_device_copy.restype = ctypes.c_int
         L.liec_device_copy.argtypes = [vp, vp, i64, vp]
         _lib = L

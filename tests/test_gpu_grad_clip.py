@@ -1,0 +1,309 @@
+"""Global gradient norm, clipping in place and clipping into rows against the definitions in 64 bits.
+
+Bounds.  The norm's sum is carried in 64 bits, so only its rounding to fp32 shows: one unit roundoff (2^-24), and 1e-12 for
+the order of the sum.  A factor is rounded once and a product once in fp32, then once to the tensor's type."""
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(__file__))
+from _gpu import DEV, GPU_MARKS, say  # noqa: E402
+from _train import DTYPES, TINY, U, U32, assert_within, generator  # noqa: E402
+
+pytestmark = GPU_MARKS
+
+
+def _tensors(N, counts, dtypes, seed, offset=0, scale=1.0):
+    """Tensors [N, n] at `offset` elements into buffers of their own, and per-worker sizes that differ."""
+    gen = generator(seed)
+    worker = 0.25 + torch.rand(N, 1, generator=gen, device=DEV)
+    out = []
+    for i, n in enumerate(counts):
+        dt = dtypes[i % len(dtypes)]
+        buf = torch.empty(N * n + offset, dtype=DTYPES[dt], device=DEV)
+        t = buf[offset:].view(N, n)
+        t.copy_(torch.randn(N, n, generator=gen, device=DEV) * worker * scale * 10.0 ** (i % 3 - 2))
+        out.append(t)
+    return out
+
+
+def _norms(tensors, N):
+    total = torch.zeros(N, dtype=torch.float64, device=DEV)
+    for t in tensors:
+        total += t.reshape(N, -1).double().square().sum(1)
+    return total.sqrt()
+
+
+def _name(t):
+    return next(k for k, v in DTYPES.items() if v == t.dtype)
+
+
+def _factors(norms, bound):
+    return torch.where(norms <= bound, torch.ones_like(norms), bound / norms)
+
+
+def _check_norms(got, want):
+    assert got.dtype == torch.float32
+    assert_within(got, want, want * (U32 + 1e-12), "norms")
+
+
+def _check_scaled(got, before, factor, N, label):
+    for i, (g, b) in enumerate(zip(got, before)):
+        u = U[_name(g)]
+        want = b.reshape(N, -1).double() * factor[:, None]
+        assert_within(g.reshape(N, -1), want, want.abs() * (3 * U32 + 1.01 * (u if u > U32 else 0.0)) + TINY[_name(g)], f"{label}, tensor {i}")
+
+
+COUNTS = {
+    "one value": [1],
+    "odd": [1, 7, 8, 9, 63, 64, 65, 8191, 8192, 8193, 3],
+    "empty among them": [0, 5, 0, 0, 16385, 0],
+    "many small": [1 + (37 * i) % 97 for i in range(300)],
+    "a launch exactly": [5] * 128,
+    "a launch and one": [5] * 128 + [40_001],
+    "an empty launch": [0] * 128 + [4099],
+    "long": [1_000_003, 77, 250_000],
+}
+
+
+@pytest.mark.parametrize("kind", list(COUNTS))
+@pytest.mark.parametrize("N", [1, 3, 8])
+@pytest.mark.parametrize("types", [("fp32",), ("bf16",), ("fp16",), ("bf16", "fp32", "fp16")])
+def test_norm_clip_and_gather(kind, N, types):
+    import paper_2402_11857_amd as pkg
+
+    say(f"case gradients {kind} N={N} {'/'.join(types)}")
+    for offset in (0, 1, 3):
+        tensors = _tensors(N, COUNTS[kind], types, seed=len(kind) + offset, offset=offset)
+        before = [t.clone() for t in tensors]
+        want = _norms(tensors, N)
+        norms = torch.full((N,), -1.0, device=DEV)
+        assert pkg.liec_grad_norm(tensors, norms) is norms
+        _check_norms(norms, want)
+        bound = float(want.median())                         # about half of the workers are clipped
+        factor = _factors(want, bound)
+        d = sum(COUNTS[kind])
+        wide = torch.full((N, d + 5), 7.0, device=DEV)
+        rows = wide[:, 2:2 + d]
+        norms.fill_(-1.0)
+        pkg.liec_gather_grads(tensors, rows, bound, norms)
+        _check_norms(norms, want)
+        assert all(torch.equal(a, b) for a, b in zip(tensors, before))
+        flat = torch.cat([t.double() for t in tensors], 1) * factor[:, None]
+        assert_within(rows, flat, flat.abs() * 3 * U32 + 2.0 ** -149, "rows")
+        assert bool((wide[:, :2] == 7.0).all()) and bool((wide[:, 2 + d:] == 7.0).all())
+        norms.fill_(-1.0)
+        pkg.liec_clip_grads(tensors, bound, norms)
+        _check_norms(norms, want)
+        _check_scaled(tensors, before, factor, N, "clip")
+        kept = (factor == 1.0) & (want < bound * (1 - 1e-6))
+        assert all(torch.equal(a[kept], b[kept]) for a, b in zip(tensors, before))
+
+
+def test_equal_calls_give_equal_bits():
+    import paper_2402_11857_amd as pkg
+
+    say("case gradients, three equal calls")
+    tensors = _tensors(5, [100_001, 3, 70_000], ("bf16",), seed=3)
+    first = pkg.liec_grad_norm(tensors)
+    assert all(torch.equal(first, pkg.liec_grad_norm(tensors)) for _ in range(2))
+
+
+def test_gather_alone_is_a_plain_copy():
+    import paper_2402_11857_amd as pkg
+
+    say("case gradients, gather without a bound")
+    tensors = _tensors(4, [9, 20_000, 1], ("fp16", "fp32"), seed=4)
+    tensors[1][2, 17] = math.nan                             # nothing is scaled, so nothing spreads
+    tensors[1][3, 5] = math.inf
+    rows = torch.empty(4, 20_010, device=DEV)
+    pkg.liec_gather_grads(tensors, rows)
+    want = torch.cat([t.float() for t in tensors], 1)
+    assert torch.equal(rows.view(torch.int32), want.view(torch.int32))
+    norms = torch.empty(4, device=DEV)
+    pkg.liec_gather_grads(tensors, rows, math.inf, norms)
+    assert torch.equal(rows.view(torch.int32), want.view(torch.int32))
+    assert norms[2].isnan() and norms[3].isinf() and norms[:2].isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_not_finite_gradients_stay_with_their_worker(dtype):
+    import paper_2402_11857_amd as pkg
+
+    say(f"case gradients, Inf and NaN, {dtype}")
+    tensors = _tensors(4, [5000, 11], (dtype,), seed=6)
+    tensors[0][1, 4321] = math.inf
+    tensors[1][2, 10] = math.nan
+    before = [t.clone() for t in tensors]
+    want = _norms(tensors, 4)
+    bound = 0.5 * float(want[0])
+    norms = torch.empty(4, device=DEV)
+    pkg.liec_clip_grads(tensors, bound, norms)
+    assert norms[1] == math.inf and norms[2].isnan()
+    _check_norms(norms[[0, 3]], want[[0, 3]])
+    factor = _factors(want, bound)
+    _check_scaled([t[[0, 3]] for t in tensors], [t[[0, 3]] for t in before], factor[[0, 3]], 2, "finite workers")
+    for t, b in zip(tensors, before):                        # an infinite norm: zeros, and NaN from Inf * 0
+        assert torch.equal(t[1].isnan(), b[1].isinf()) and bool((t[1][~b[1].isinf()] == 0).all())
+        assert t[2].isnan().all()
+
+
+def test_zero_bounds_and_zero_gradients():
+    import paper_2402_11857_amd as pkg
+
+    say("case gradients, bounds of 0 and Inf, gradients of 0")
+    tensors = [torch.zeros(2, 1000, device=DEV), torch.zeros(2, 3, device=DEV)]
+    tensors[0][1] = 1.0
+    norms = torch.empty(2, device=DEV)
+    pkg.liec_clip_grads(tensors, math.inf, norms)
+    assert norms[0] == 0 and abs(float(norms[1]) - math.sqrt(1000)) < 4e-6 and bool((tensors[0][1] == 1).all())
+    pkg.liec_clip_grads(tensors, 0.0)
+    assert all(bool((t == 0).all()) for t in tensors)
+
+
+@pytest.mark.parametrize("value", [1e30, 1e-30, 3e38])
+def test_sums_neither_overflow_nor_vanish(value):
+    import paper_2402_11857_amd as pkg
+
+    say(f"case gradients of {value}")
+    t = torch.full((2, 100), value, device=DEV)
+    norms = pkg.liec_grad_norm([t])
+    want = _norms([t], 2)
+    if float(want[0]) < 3.4e38:
+        _check_norms(norms, want)
+    else:
+        assert norms.isinf().all()                           # the norm itself is beyond fp32; the factor is not
+    bound = value
+    pkg.liec_clip_grads([t], bound)
+    assert_within(t, torch.full_like(t, value, dtype=torch.float64) * bound / want[:, None], torch.tensor(3 * U32 * value, device=DEV), "clipped")
+
+
+def test_strided_and_shared_tensors():
+    import paper_2402_11857_amd as pkg
+
+    say("case gradients, columns of a matrix, workers in reverse, shared tensors")
+    rows = torch.randn(4, 1003, generator=generator(8), device=DEV)
+    views = [rows[:, 1:300], rows[:, 300:301], rows[:, 400:1003]]
+    want = _norms(views, 4)
+    _check_norms(pkg.liec_grad_norm(views), want)
+    before = [v.clone() for v in views]
+    rest = rows[:, 301:400].clone()
+    pkg.liec_clip_grads(views, 3.0)
+    _check_scaled(views, before, _factors(want, 3.0), 4, "columns")
+    assert torch.equal(rows[:, 301:400], rest)
+    shared = torch.randn(700, generator=generator(9), device=DEV).expand(4, 700)
+    _check_norms(pkg.liec_grad_norm([shared]), _norms([shared], 4))
+    out = torch.empty(4, 700, device=DEV)
+    pkg.liec_gather_grads([shared], out)
+    assert torch.equal(out, shared)
+    # columns of the matrix whose other columns are gathered into
+    wide = torch.randn(4, 200, generator=generator(10), device=DEV)
+    pkg.liec_gather_grads([wide[:, 100:160]], wide[:, 20:80])
+    assert torch.equal(wide[:, 20:80], wide[:, 100:160])
+
+
+def test_tensors_of_one_worker_of_any_shape():
+    import paper_2402_11857_amd as pkg
+
+    say("case gradients of one worker")
+    tensors = [torch.randn(3, 5, 7, generator=generator(11), device=DEV), torch.randn(1, generator=generator(12), device=DEV),
+               torch.tensor(2.0, device=DEV)]
+    want = torch.cat([t.reshape(-1) for t in tensors]).double().norm().reshape(1)
+    _check_norms(pkg.liec_grad_norm(tensors, workers=1), want)
+    before = [t.clone() for t in tensors]
+    pkg.liec_clip_grads(tensors, 1.0, workers=1)
+    _check_scaled([t.reshape(1, -1) for t in tensors], [t.reshape(1, -1) for t in before], 1.0 / want, 1, "one worker")
+
+
+def test_no_tensors():
+    import paper_2402_11857_amd as pkg
+
+    say("case gradients, none")
+    norms = torch.full((3,), -1.0, device=DEV)
+    pkg.liec_grad_norm([], norms)
+    assert bool((norms == 0).all())
+    norms.fill_(-1.0)
+    pkg.liec_clip_grads([torch.empty(3, 0, device=DEV)], 1.0, norms)
+    assert bool((norms == 0).all())
+    norms.fill_(-1.0)
+    pkg.liec_gather_grads([], torch.empty(3, 0, device=DEV), 1.0, norms)
+    assert bool((norms == 0).all())
+
+
+def test_values_beyond_32_bit_offsets():
+    import paper_2402_11857_amd as pkg
+
+    n = (1 << 31) + 8201
+    say(f"case gradients, one bf16 tensor of {n} values")
+    t = torch.zeros(1, n, dtype=torch.bfloat16, device=DEV)
+    t[0, -3:] = 3.0
+    t[0, 1 << 31] = 4.0
+    t[0, 5] = 6.0
+    norms = pkg.liec_grad_norm([t])
+    assert abs(float(norms[0]) - math.sqrt(79.0)) <= U32 * 9
+    pkg.liec_clip_grads([t], math.sqrt(79.0) / 2)
+    assert t[0, -3:].tolist() == [1.5] * 3 and float(t[0, 1 << 31]) == 2.0 and float(t[0, 5]) == 3.0
+
+
+def test_another_stream_and_graph_replays():
+    import paper_2402_11857_amd as pkg
+
+    say("case gradients on another stream, in a graph")
+    tensors = _tensors(3, [40_000, 17], ("bf16",), seed=13)
+    rows, norms = torch.empty(3, 40_017, device=DEV), torch.empty(3, device=DEV)
+    bound = float(_norms(tensors, 3).median())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        pkg.liec_gather_grads(tensors, rows, bound, norms)
+    side.synchronize()
+    want_rows, want_norms = rows.clone(), norms.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        pkg.liec_gather_grads(tensors, rows, bound, norms)
+    for k in range(3):
+        rows.zero_()
+        norms.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(rows, want_rows) and torch.equal(norms, want_norms), f"replay {k}"
+    tensors[0].mul_(2.0)                                     # a replay works on what the tensors hold then
+    graph.replay()
+    eager = pkg.liec_grad_norm(tensors)
+    torch.cuda.synchronize()
+    assert torch.equal(norms, eager)
+
+
+def test_refusals():
+    import paper_2402_11857_amd as pkg
+
+    say("case gradients, refusals")
+    a = torch.ones(2, 100, device=DEV)
+    rows = torch.empty(2, 100, device=DEV)
+    for bad in (lambda: pkg.liec_grad_norm([a.cpu()]),
+                lambda: pkg.liec_grad_norm([a.double()]),
+                lambda: pkg.liec_grad_norm([a], torch.empty(2, dtype=torch.float64, device=DEV)),
+                lambda: pkg.liec_gather_grads([a], rows.double()),
+                lambda: pkg.liec_grad_norm([a, a.cpu()])):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: pkg.liec_grad_norm([]),
+                lambda: pkg.liec_grad_norm([a, torch.ones(3, 4, device=DEV)]),
+                lambda: pkg.liec_grad_norm([a[:, ::2]]),
+                lambda: pkg.liec_grad_norm([a.t()], workers=1),
+                lambda: pkg.liec_grad_norm([a], workers=2),
+                lambda: pkg.liec_grad_norm([a], torch.empty(3, device=DEV)),
+                lambda: pkg.liec_gather_grads([a], rows[:, :99])):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: pkg.liec_clip_grads([a], -1.0),
+                lambda: pkg.liec_clip_grads([a], math.nan),
+                lambda: pkg.liec_clip_grads([a, a], 1.0),                            # a tied tensor listed twice
+                lambda: pkg.liec_clip_grads([torch.ones(5, device=DEV).expand(2, 5)], 1.0),
+                lambda: pkg.liec_gather_grads([a], a)):
+        with pytest.raises(pkg.LiecError):
+            bad()
+    assert bool((a == 1).all())
