@@ -50,7 +50,7 @@ int64_t liec_grads_workspace(int32_t N, int32_t T);
 /*
  * liec_grad_norm: norms[i] = sqrt(sum over the T tensors of the squares of worker i's values), i < N (DEVICE, fp32,
  * N values).  Infinities and NaN show in the norm of their worker, and only there.  T = 0 or no values: zero.
- *   1 <= N <= 65535, 0 <= T <= LIEC_GRAD_MAX_TENSORS, at most 2^44 values per worker.  stride may be anything, 0
+ *   1 <= N <= 65535, 0 <= T <= LIEC_GRAD_MAX_TENSORS, at most 2^35 values per worker.  stride may be anything, 0
  *   included (workers that share a tensor).  Two kernels (one more for each further 128 tensors).
  */
 liec_status liec_grad_norm(const liec_grad_tensor *tensors, int32_t T, int32_t N, float *norms, void *workspace,

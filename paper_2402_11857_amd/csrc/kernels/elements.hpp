@@ -1,4 +1,4 @@
-// Element types of the operators around a backward pass (fp32, bf16, fp16): vectors of 16 bytes and of 8 values, read from
+// Element types of the operators around a backward pass (fp32, bf16, fp16): vectors of 16 bytes, read from
 // and written to any address that is a multiple of the element's size, computed on in fp32.
 #pragma once
 #include "common.hpp"
@@ -118,34 +118,25 @@ __device__ __forceinline__ void st16(T* p, v4u v) {
     else *reinterpret_cast<any*>(p) = (any)v;
 }
 
-// 8 consecutive values as they are in memory (16 bytes, or 32 of fp32).
+// keep: the same for the whole launch.  The empty statements hold the two stores apart: the compiler would make them one,
+// a plain one.
 template <typename T>
-struct Raw8 {
-    v4u w;
-    __device__ __forceinline__ void load(const T* p) { w = ld16<T, false>(p); }
-    __device__ __forceinline__ void load_stream(const T* p) { w = ld16<T, true>(p); }
-    __device__ __forceinline__ void widen(float (&f)[8]) const { Vec16<T>::widen(w, f); }
-    static __device__ __forceinline__ void store(T* p, const float (&f)[8]) { st16<T, true>(p, Vec16<T>::narrow(f)); }
-};
-template <>
-struct Raw8<float> {
-    v4u w, z;
-    __device__ __forceinline__ void load(const float* p) {
-        w = ld16<float, false>(p);
-        z = ld16<float, false>(p + 4);
+__device__ __forceinline__ void st16_as(bool keep, T* p, v4u v) {
+    if (keep) {
+        asm volatile("");
+        st16<T, false>(p, v);
+        asm volatile("");
+    } else {
+        st16<T, true>(p, v);
     }
-    __device__ __forceinline__ void load_stream(const float* p) {
-        w = ld16<float, true>(p);
-        z = ld16<float, true>(p + 4);
-    }
-    __device__ __forceinline__ void widen(float (&f)[8]) const {
-        f[0] = __uint_as_float(w.x); f[1] = __uint_as_float(w.y); f[2] = __uint_as_float(w.z); f[3] = __uint_as_float(w.w);
-        f[4] = __uint_as_float(z.x); f[5] = __uint_as_float(z.y); f[6] = __uint_as_float(z.z); f[7] = __uint_as_float(z.w);
-    }
-    static __device__ __forceinline__ void store(float* p, const float (&f)[8]) {
-        st16<float, true>(p, v4u{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])});
-        st16<float, true>(p + 4, v4u{__float_as_uint(f[4]), __float_as_uint(f[5]), __float_as_uint(f[6]), __float_as_uint(f[7])});
-    }
+}
+
+// 4 values of 16 bits as one streaming load.
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint32_t v2u_any2 __attribute__((ext_vector_type(2), aligned(2)));
+template <typename T>
+struct Half16 {
+    static __device__ __forceinline__ v2u load(const T* p) { return (v2u)__builtin_nontemporal_load(reinterpret_cast<const v2u_any2*>(p)); }
 };
 
 }  // namespace liec

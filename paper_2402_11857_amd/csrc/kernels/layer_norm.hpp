@@ -4,16 +4,18 @@
 //   backward   h_j = (x_j - mu) rstd,  a_j = dy_j w_j,  dx_j = rstd (a_j - mean a - h_j mean(a h))
 //              dw_j = sum over the worker's rows of dy_j h_j,  db_j = sum over them of dy_j
 //
-// A team of TEAM lanes holds one row in registers, K vectors of 8 columns per lane, so that a row is read once; teams of up
+// A team of TEAM lanes holds one row in registers, K vectors of 16 bytes per lane, so that a row is read once; teams of up
 // to a wave add up inside the wave, larger ones through LDS.  All sums are fp32, of at most a few hundred terms in a chain.
-// The last vector of a row that is not a multiple of 8 columns long starts 8 columns before the row's end: what it shares
-// with the vector before it is left out of the sums and stored twice with the same value, and no access needs a branch.
+// The last vector of a row that is not a multiple of a vector long starts a vector's length before the row's end: what it
+// shares with the vector before it is left out of the sums and stored twice with the same value, and no access needs a branch.
 #pragma once
+#include <type_traits>
+
 #include "elements.hpp"
 
 namespace liec {
 
-constexpr int kLnVec = 8;
+constexpr int kLnShortest = 8;         // columns of the shortest row that a team holds
 constexpr int kLnWide = 1024;          // threads that walk a row too long (or too short) for registers
 
 struct LnRows {                        // a [workers, rows, columns] tensor of unit column stride
@@ -24,6 +26,12 @@ struct LnParam {                       // a [workers, columns] tensor of unit co
     void* data;
     int64_t stride;
     uint32_t type;
+};
+
+// Rows of a thread block: from blockIdx.x * pitch on, at most `span` of them, a team's own at distances of `step`.
+struct LnWalk {
+    int64_t pitch, span, step;
+    bool keep;                         // results are left in the caches for whoever reads them next
 };
 
 // ---- sums over a team --------------------------------------------------------------------------------------------
@@ -40,12 +48,12 @@ __device__ __forceinline__ float add_lane32(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __fadd_rn(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-// Sum over groups of W lanes (8 .. 64), the same bits in every lane of the group.
+// Sum over groups of W lanes (2 .. 64), the same bits in every lane of the group.
 template <int W>
 __device__ __forceinline__ float lanes_sum(float v) {
     v += dpp_move<0xb1>(v);                      // quad_perm 1 0 3 2
-    v += dpp_move<0x4e>(v);                      // quad_perm 2 3 0 1
-    v += dpp_move<0x141>(v);                     // row_half_mirror: the other quad of 8 lanes
+    if (W >= 4) v += dpp_move<0x4e>(v);          // quad_perm 2 3 0 1
+    if (W >= 8) v += dpp_move<0x141>(v);         // row_half_mirror: the other quad of 8 lanes
     if (W >= 16) v += dpp_move<0x140>(v);        // row_mirror: the other half of 16
     if (W >= 32) v = add_lane16(v);
     if (W >= 64) v = add_lane32(v);
@@ -61,138 +69,137 @@ __device__ __forceinline__ float groups_sum(float v) {
 }
 
 // This lane's vector k of a row of C columns: where it starts, and how many of its first columns belong to the vector before
-// it (8 or more: the vector lies beyond the row).  Needs C >= 8.
-template <int TEAM>
+// it (V or more: the vector lies beyond the row).  A FULL row ends with the team's last vector.
+template <int TEAM, int V, bool FULL>
 __device__ __forceinline__ uint32_t vec_start(uint32_t l, int k, uint32_t C, uint32_t& skip) {
-    const uint32_t c = (k * TEAM + l) * kLnVec, s = min(c, C - kLnVec);
+    const uint32_t c = (k * TEAM + l) * V, s = FULL ? c : min(c, C - V);
     skip = c - s;
     return s;
 }
+// Element `at` of a row.  For whole waves on one row the row's address is scalar and `at` the only part that a lane holds.
+template <typename T>
+__device__ __forceinline__ T* in_row(T* row, uint32_t at) {
+    typedef typename std::conditional<std::is_const<T>::value, const char, char>::type byte;
+    return reinterpret_cast<T*>(reinterpret_cast<byte*>(row) + (uint32_t)(at * sizeof(T)));
+}
+// The team that a thread belongs to, known to be the same for a whole wave where it is.
+template <int TEAM>
+__device__ __forceinline__ uint32_t team_index() {
+    return TEAM >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : threadIdx.x / TEAM;
+}
+// Whether vector k may lie at or beyond the end of its row: rows that half as many vectors per lane hold take a smaller team,
+// except for the smallest one.
+template <int TEAM, int K, bool FULL>
+constexpr bool may_end(int k) { return !FULL && (TEAM == 8 || k >= K / 2); }
 
-__device__ __forceinline__ void load_param(const LnParam& p, uint32_t worker, uint32_t col, float absent, float (&f)[8]) {
+template <int V>
+__device__ __forceinline__ void load_param(const LnParam& p, uint32_t worker, uint32_t col, float absent, float (&f)[V]) {
     if (!p.data) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = absent;
+        for (int j = 0; j < V; ++j) f[j] = absent;
         return;
     }
     const int64_t at = (int64_t)worker * p.stride + col;
-    if (p.type == kF32) {
-        Raw8<float> r;
-        r.load(static_cast<const float*>(p.data) + at);
-        r.widen(f);
-    } else if (p.type == kBF16) {
-        Raw8<bf16> r;
-        r.load(static_cast<const bf16*>(p.data) + at);
-        r.widen(f);
-    } else {
-        Raw8<f16> r;
-        r.load(static_cast<const f16*>(p.data) + at);
-        r.widen(f);
-    }
+    auto load = [&](auto* from) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] = widen(from[at + j]);
+    };
+    if (p.type == kF32) load(static_cast<const float*>(p.data));
+    else if (p.type == kBF16) load(static_cast<const bf16*>(p.data));
+    else load(static_cast<const f16*>(p.data));
 }
 
 // ---- forward -------------------------------------------------------------------------------------------------------
-// Block (strip, worker): rows strip * per .. of the worker, TEAM lanes to a row.
-template <typename T, int TEAM, int K>
-__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_forward(uint32_t C, uint32_t per, float eps, int64_t R, float* __restrict__ mean,
-                                                                                float* __restrict__ rstd, LnRows x, LnRows y, LnParam w, LnParam b) {
-    constexpr int THREADS = TEAM > 64 ? TEAM : kBlock, TEAMS = THREADS / TEAM, WAVES = TEAM > 64 ? TEAM / 64 : 1;
-    __shared__ float lds[2][3][WAVES > 1 ? WAVES : 1];
-    const uint32_t worker = blockIdx.y, l = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    const int64_t begin = (int64_t)blockIdx.x * per, end = min(begin + (int64_t)per, R);
+// Block (strip, worker): rows strip * per .. of the worker, TEAM lanes to a row, the next row of a team requested ahead.
+template <typename T, int TEAM, int K, bool FULL>
+__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_forward(uint32_t C, float eps, int64_t R, LnWalk walk, float* __restrict__ mean,
+                                                                            float* __restrict__ rstd, LnRows x, LnRows y, LnParam w, LnParam b) {
+    constexpr int WAVES = TEAM > 64 ? TEAM / 64 : 1, V = Vec16<T>::n;
+    constexpr int LANES = TEAM > 64 ? 64 : TEAM;
+    __shared__ float lds[2][2][WAVES];
+    const uint32_t worker = blockIdx.y, l = threadIdx.x % TEAM, team = team_index<TEAM>(), wave = l >> 6;
+    const int64_t begin = (int64_t)blockIdx.x * walk.pitch, first = begin + team, end = min(begin + walk.span, R), step = walk.step;
     const T* const xs = static_cast<const T*>(x.data) + (int64_t)worker * x.worker;
     T* const ys = static_cast<T*>(y.data) + (int64_t)worker * y.worker;
+    const int64_t stat = (int64_t)worker * R;
     uint32_t at[K], skip[K];
-    float wv[K][8], bv[K][8];
 #pragma unroll
-    for (int k = 0; k < K; ++k) at[k] = vec_start<TEAM>(l, k, C, skip[k]);
-    int64_t r = begin + team;
-    Raw8<T> raw[K];
-    if (r < end) {
+    for (int k = 0; k < K; ++k) at[k] = vec_start<TEAM, V, FULL>(l, k, C, skip[k]);
+    v4u held[K];
+    if (first < end) {
 #pragma unroll
-        for (int k = 0; k < K; ++k) raw[k].load_stream(xs + r * x.row + at[k]);
+        for (int k = 0; k < K; ++k) held[k] = ld16<T, true>(in_row(xs + first * x.row, at[k]));
     }
+    float wv[K][V], bv[K][V];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        load_param(w, worker, at[k], 1.f, wv[k]);
-        load_param(b, worker, at[k], 0.f, bv[k]);
+        load_param<V>(w, worker, at[k], 1.f, wv[k]);
+        load_param<V>(b, worker, at[k], 0.f, bv[k]);
     }
     const float inv = 1.f / (float)C;
-    // columns that this lane's wave (of a team of several) counts, for the waves' means
-    const uint32_t wave = l >> 6;
+    // columns of this lane's wave, and of the wave whose sums this lane puts together
+    const uint32_t other = l & (WAVES - 1);
+    float mine = 0.f, others = 0.f, mine_inv = inv, others_inv = 0.f;
+    if (WAVES > 1) {
+        uint32_t left_out = 0;
+#pragma unroll
+        for (int k = 0; k < K; ++k) left_out += min(skip[k], (uint32_t)V);
+        mine = lanes_sum<64>((float)(K * V - left_out));
+        if ((l & 63) == 0) lds[1][0][wave] = mine;
+        __syncthreads();
+        others = lds[1][0][other];
+        mine_inv = 1.f / fmaxf(mine, 1.f);
+        others_inv = 1.f / fmaxf(others, 1.f);
+    }
     uint32_t parity = 0;
-    for (; r < end; r += TEAMS) {
-        float f[K][8];
+    for (int64_t r = first; r < end; r += step) {
+        float f[K][V];
 #pragma unroll
-        for (int k = 0; k < K; ++k) raw[k].widen(f[k]);
-        if (r + TEAMS < end) {
+        for (int k = 0; k < K; ++k) Vec16<T>::widen(held[k], f[k]);
+        if (r + step < end) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) raw[k].load_stream(xs + (r + TEAMS) * x.row + at[k]);
+            for (int k = 0; k < K; ++k) held[k] = ld16<T, true>(in_row(xs + (r + step) * x.row, at[k]));
         }
-        float s = 0.f;
+        float s = 0.f, m2 = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s += (uint32_t)j >= skip[k] ? f[k][j] : 0.f;
-        float mu, m2 = 0.f;
-        if (WAVES == 1) {
-            mu = lanes_sum<(TEAM > 64 ? 64 : TEAM)>(s) * inv;
+            for (int j = 0; j < V; ++j) s += !may_end<TEAM, K, FULL>(k) || (uint32_t)j >= skip[k] ? f[k][j] : 0.f;
+        s = lanes_sum<LANES>(s);
+        // squares around the row's mean, or around the wave's own
+        float mu = s * mine_inv;
 #pragma unroll
-            for (int k = 0; k < K; ++k)
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float d = f[k][j] - mu;
-                    m2 = (uint32_t)j >= skip[k] ? __fmaf_rn(d, d, m2) : m2;
-                }
-            m2 = lanes_sum<(TEAM > 64 ? 64 : TEAM)>(m2);
-        } else {
-            // every wave's own sum and its squares around its own mean, put together as sums of squares around the row's mean
-            s = lanes_sum<64>(s);
-            uint32_t mine = 0;
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                const uint32_t c0 = (k * TEAM + wave * 64) * kLnVec;
-                mine += c0 < C ? min(C - c0, 64u * kLnVec) : 0u;
+            for (int j = 0; j < V; ++j) {
+                const float d = f[k][j] - mu;
+                m2 = !may_end<TEAM, K, FULL>(k) || (uint32_t)j >= skip[k] ? __fmaf_rn(d, d, m2) : m2;
             }
-            const float own = mine ? s / (float)mine : 0.f;
-#pragma unroll
-            for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float d = f[k][j] - own;
-                    m2 = (uint32_t)j >= skip[k] ? __fmaf_rn(d, d, m2) : m2;
-                }
-            m2 = lanes_sum<64>(m2);
+        m2 = lanes_sum<LANES>(m2);
+        if (WAVES > 1) {
+            // waves' sums of squares around their own means, put together around the row's
             if ((l & 63) == 0) {
                 lds[parity][0][wave] = s;
                 lds[parity][1][wave] = m2;
-                lds[parity][2][wave] = (float)mine;
             }
             __syncthreads();
-            float total = 0.f;
-#pragma unroll
-            for (int q = 0; q < WAVES; ++q) total += lds[parity][0][q];
-            mu = total * inv;
-            m2 = 0.f;
-#pragma unroll
-            for (int q = 0; q < WAVES; ++q) {
-                const float cnt = lds[parity][2][q];
-                const float d = cnt > 0.f ? lds[parity][0][q] / cnt - mu : 0.f;
-                m2 += __fmaf_rn(cnt * d, d, lds[parity][1][q]);
-            }
+            const float sq = lds[parity][0][other], mq = lds[parity][1][other];
+            mu = lanes_sum<WAVES>(sq) * inv;
+            const float d = __fmaf_rn(sq, others_inv, -mu);
+            m2 = lanes_sum<WAVES>(__fmaf_rn(others * d, d, mq));
             parity ^= 1;
         }
         const float rs = rsqrtf(__fmaf_rn(m2, inv, eps));
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            float o[8];
+            float o[V];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = __fmaf_rn((f[k][j] - mu) * rs, wv[k][j], bv[k][j]);
-            if (skip[k] < kLnVec) Raw8<T>::store(ys + r * y.row + at[k], o);
+            for (int j = 0; j < V; ++j) o[j] = __fmaf_rn((f[k][j] - mu) * rs, wv[k][j], bv[k][j]);
+            if (!may_end<TEAM, K, FULL>(k) || skip[k] < V) st16_as<T>(walk.keep, in_row(ys + r * y.row, at[k]), Vec16<T>::narrow(o));
         }
         if (l == 0) {
-            if (mean) mean[(int64_t)worker * R + r] = mu;
-            if (rstd) rstd[(int64_t)worker * R + r] = rs;
+            if (mean) mean[stat + r] = mu;
+            if (rstd) rstd[stat + r] = rs;
         }
     }
 }
@@ -235,57 +242,60 @@ __global__ __launch_bounds__(kLnWide) void k_ln_forward_wide(int64_t C, float ep
 
 // ---- backward ------------------------------------------------------------------------------------------------------
 // Block (strip, worker): dx of its rows, and their share of dw and db in registers, which it leaves in partial[worker][strip]
-// (2 x C values), or in dw and db themselves where it is the only one (partial == nullptr).
-template <typename T, int TEAM, int K>
-__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_backward(uint32_t C, uint32_t per, int64_t R, float* __restrict__ partial,
-                                                                                 const float* __restrict__ mean, const float* __restrict__ rstd, LnRows dy,
-                                                                                 LnRows x, LnRows dx, LnParam w, LnParam dw, LnParam db) {
-    constexpr int THREADS = TEAM > 64 ? TEAM : kBlock, TEAMS = THREADS / TEAM, WAVES = TEAM > 64 ? TEAM / 64 : 1;
-    constexpr int COLS = TEAM <= 64 ? TEAM * K * kLnVec : 1;
+// (2 x C values), or in dw and db themselves where it is the only one (partial == nullptr).  The next P rows of a
+// team are requested ahead.
+template <typename T, int TEAM, int K, bool FULL, int P>
+__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock), (K * Vec16<T>::n == 8 || TEAM == 1024 ? 4 : 2)) void k_ln_backward(uint32_t C, int64_t R, LnWalk walk, float* __restrict__ partial,
+                                                                                const float* __restrict__ mean, const float* __restrict__ rstd, LnRows dy,
+                                                                                LnRows x, LnRows dx, LnParam w, LnParam dw, LnParam db) {
+    constexpr int WAVES = TEAM > 64 ? TEAM / 64 : 1, V = Vec16<T>::n;
+    constexpr int LANES = TEAM > 64 ? 64 : TEAM, COLS = TEAM <= 64 ? TEAM * K * V : 1;
     __shared__ float lds[2][2][WAVES];
     __shared__ __align__(16) float sums[2][COLS];
-    const uint32_t worker = blockIdx.y, l = threadIdx.x % TEAM, team = threadIdx.x / TEAM;
-    const int64_t begin = (int64_t)blockIdx.x * per, end = min(begin + (int64_t)per, R);
+    const uint32_t worker = blockIdx.y, l = threadIdx.x % TEAM, team = team_index<TEAM>();
+    const int64_t begin = (int64_t)blockIdx.x * walk.pitch, first = begin + team, end = min(begin + walk.span, R), step = walk.step;
     const T* const xs = static_cast<const T*>(x.data) + (int64_t)worker * x.worker;
     const T* const gs = static_cast<const T*>(dy.data) + (int64_t)worker * dy.worker;
     T* const os = static_cast<T*>(dx.data) + (int64_t)worker * dx.worker;
     const float* const mus = mean + (int64_t)worker * R;
     const float* const rss = rstd + (int64_t)worker * R;
     uint32_t at[K], skip[K];
-    float wv[K][8], aw[K][8], ab[K][8];
+    float wv[K][V], aw[K][V], ab[K][V];
 #pragma unroll
-    for (int k = 0; k < K; ++k) at[k] = vec_start<TEAM>(l, k, C, skip[k]);
-    int64_t r = begin + team;
-    Raw8<T> rx[K], rg[K];
-    float mu = 0.f, rs = 0.f;
-    if (r < end) {
+    for (int k = 0; k < K; ++k) at[k] = vec_start<TEAM, V, FULL>(l, k, C, skip[k]);
+    v4u rx[P][K], rg[P][K];
+    float mu[P], rs[P];
+    auto request = [&](int64_t r, v4u (&vx)[K], v4u (&vg)[K], float& m, float& s) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            rx[k].load_stream(xs + r * x.row + at[k]);
-            rg[k].load_stream(gs + r * dy.row + at[k]);
+            vx[k] = ld16<T, true>(in_row(xs + r * x.row, at[k]));
+            vg[k] = ld16<T, true>(in_row(gs + r * dy.row, at[k]));
         }
-        mu = mus[r];
-        rs = rss[r];
-    }
+        m = mus[r];
+        s = rss[r];
+    };
+#pragma unroll
+    for (int q = 0; q < P; ++q)
+        if (first + q * step < end) request(first + q * step, rx[q], rg[q], mu[q], rs[q]);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        load_param(w, worker, at[k], 1.f, wv[k]);
+        load_param<V>(w, worker, at[k], 1.f, wv[k]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) aw[k][j] = ab[k][j] = 0.f;
+        for (int j = 0; j < V; ++j) aw[k][j] = ab[k][j] = 0.f;
     }
     const float inv = 1.f / (float)C;
     uint32_t parity = 0;
-    for (; r < end; r += TEAMS) {
-        float h[K][8], a[K][8], s1 = 0.f, s2 = 0.f;
+    auto row = [&](int64_t r, v4u (&vx)[K], v4u (&vg)[K], float& m, float& s) {
+        float h[K][V], a[K][V], s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            float g[8];
-            rx[k].widen(h[k]);
-            rg[k].widen(g);
+            float g[V];
+            Vec16<T>::widen(vx[k], h[k]);
+            Vec16<T>::widen(vg[k], g);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const bool in = (uint32_t)j >= skip[k];
-                h[k][j] = (h[k][j] - mu) * rs;
+            for (int j = 0; j < V; ++j) {
+                const bool in = !may_end<TEAM, K, FULL>(k) || (uint32_t)j >= skip[k];
+                h[k][j] = (h[k][j] - m) * s;
                 a[k][j] = g[j] * wv[k][j];
                 ab[k][j] += in ? g[j] : 0.f;
                 aw[k][j] = in ? __fmaf_rn(g[j], h[k][j], aw[k][j]) : aw[k][j];
@@ -293,42 +303,35 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_backward(uin
                 s2 = in ? __fmaf_rn(a[k][j], h[k][j], s2) : s2;
             }
         }
-        const float rs_now = rs;
-        if (r + TEAMS < end) {
-#pragma unroll
-            for (int k = 0; k < K; ++k) {
-                rx[k].load_stream(xs + (r + TEAMS) * x.row + at[k]);
-                rg[k].load_stream(gs + (r + TEAMS) * dy.row + at[k]);
-            }
-            mu = mus[r + TEAMS];
-            rs = rss[r + TEAMS];
-        }
-        s1 = lanes_sum<(TEAM > 64 ? 64 : TEAM)>(s1);
-        s2 = lanes_sum<(TEAM > 64 ? 64 : TEAM)>(s2);
+        const float rs_now = s;
+        if (r + P * step < end) request(r + P * step, vx, vg, m, s);
+        s1 = lanes_sum<LANES>(s1);
+        s2 = lanes_sum<LANES>(s2);
         if (WAVES > 1) {
             if ((l & 63) == 0) {
                 lds[parity][0][l >> 6] = s1;
                 lds[parity][1][l >> 6] = s2;
             }
             __syncthreads();
-            s1 = s2 = 0.f;
-#pragma unroll
-            for (int q = 0; q < WAVES; ++q) {
-                s1 += lds[parity][0][q];
-                s2 += lds[parity][1][q];
-            }
+            s1 = lanes_sum<WAVES>(lds[parity][0][l & (WAVES - 1)]);
+            s2 = lanes_sum<WAVES>(lds[parity][1][l & (WAVES - 1)]);
             parity ^= 1;
         }
         const float c1 = s1 * inv, c2 = s2 * inv;
         if (dx.data) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float o[8];
+                float o[V];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = rs_now * __fmaf_rn(-h[k][j], c2, a[k][j] - c1);
-                if (skip[k] < kLnVec) Raw8<T>::store(os + r * dx.row + at[k], o);
+                for (int j = 0; j < V; ++j) o[j] = rs_now * __fmaf_rn(-h[k][j], c2, a[k][j] - c1);
+                if (!may_end<TEAM, K, FULL>(k) || skip[k] < V) st16_as<T>(walk.keep, in_row(os + r * dx.row, at[k]), Vec16<T>::narrow(o));
             }
         }
+    };
+    for (int64_t r = first; r < end; r += P * step) {
+#pragma unroll
+        for (int q = 0; q < P; ++q)
+            if (r + q * step < end) row(r + q * step, rx[q], rg[q], mu[q], rs[q]);
     }
     if (!dw.data && !db.data) return;
     float* const out = partial ? partial + ((size_t)worker * gridDim.x + blockIdx.x) * 2 * C : nullptr;
@@ -337,18 +340,18 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_backward(uin
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
+            for (int j = 0; j < V; ++j) {
                 aw[k][j] = groups_sum<TEAM>(aw[k][j]);
                 ab[k][j] = groups_sum<TEAM>(ab[k][j]);
             }
         for (uint32_t q = 0; q < kBlock / 64; ++q) {
-            if ((threadIdx.x >> 6) == q && (threadIdx.x & 63) < (TEAM > 64 ? 64 : TEAM)) {
+            if ((threadIdx.x >> 6) == q && (threadIdx.x & 63) < LANES) {
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    float* const sw = &sums[0][(k * TEAM + l) * kLnVec];
-                    float* const sb = &sums[1][(k * TEAM + l) * kLnVec];
+                    float* const sw = &sums[0][(k * TEAM + l) * V];
+                    float* const sb = &sums[1][(k * TEAM + l) * V];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
+                    for (int j = 0; j < V; ++j) {
                         sw[j] = q ? sw[j] + aw[k][j] : aw[k][j];
                         sb[j] = q ? sb[j] + ab[k][j] : ab[k][j];
                     }
@@ -358,7 +361,7 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_backward(uin
         }
         for (uint32_t c = threadIdx.x; c < C; c += kBlock) {
             // column c is where its vector put it: the last vector of a row starts early
-            const uint32_t v = c / kLnVec, s = min(v * kLnVec, C - kLnVec), i = v * kLnVec + (c - s);
+            const uint32_t v = c / V, s = min(v * V, C - V), i = v * V + (c - s);
             const float sw = sums[0][i], sb = sums[1][i];
             if (out) {
                 out[c] = sw;
@@ -368,25 +371,27 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_backward(uin
                 if (db.data) store_any(db.data, (int64_t)worker * db.stride + c, db.type, sb);
             }
         }
-    } else {
+        return;
+    }
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
             if (out && skip[k] == 0) {
-                st16<float, false>(out + at[k], v4u{__float_as_uint(aw[k][0]), __float_as_uint(aw[k][1]), __float_as_uint(aw[k][2]), __float_as_uint(aw[k][3])});
-                st16<float, false>(out + at[k] + 4, v4u{__float_as_uint(aw[k][4]), __float_as_uint(aw[k][5]), __float_as_uint(aw[k][6]), __float_as_uint(aw[k][7])});
-                st16<float, false>(out + C + at[k], v4u{__float_as_uint(ab[k][0]), __float_as_uint(ab[k][1]), __float_as_uint(ab[k][2]), __float_as_uint(ab[k][3])});
-                st16<float, false>(out + C + at[k] + 4, v4u{__float_as_uint(ab[k][4]), __float_as_uint(ab[k][5]), __float_as_uint(ab[k][6]), __float_as_uint(ab[k][7])});
-            } else {
+                const uint32_t c = at[k] + j;
+                st16<float, false>(out + c, v4u{__float_as_uint(aw[k][j]), __float_as_uint(aw[k][j + 1]), __float_as_uint(aw[k][j + 2]), __float_as_uint(aw[k][j + 3])});
+                st16<float, false>(out + C + c, v4u{__float_as_uint(ab[k][j]), __float_as_uint(ab[k][j + 1]), __float_as_uint(ab[k][j + 2]), __float_as_uint(ab[k][j + 3])});
+                continue;
+            }
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    if ((uint32_t)j < skip[k]) continue;
-                    if (out) {
-                        out[at[k] + j] = aw[k][j];
-                        out[C + at[k] + j] = ab[k][j];
-                    } else {
-                        if (dw.data) store_any(dw.data, (int64_t)worker * dw.stride + at[k] + j, dw.type, aw[k][j]);
-                        if (db.data) store_any(db.data, (int64_t)worker * db.stride + at[k] + j, db.type, ab[k][j]);
-                    }
+            for (int i = j; i < j + 4; ++i) {
+                if ((uint32_t)i < skip[k]) continue;
+                if (out) {
+                    out[at[k] + i] = aw[k][i];
+                    out[C + at[k] + i] = ab[k][i];
+                } else {
+                    if (dw.data) store_any(dw.data, (int64_t)worker * dw.stride + at[k] + i, dw.type, aw[k][i]);
+                    if (db.data) store_any(db.data, (int64_t)worker * db.stride + at[k] + i, db.type, ab[k][i]);
                 }
             }
         }

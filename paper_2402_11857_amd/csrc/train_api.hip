@@ -16,9 +16,17 @@ using namespace liec;
 namespace {
 
 constexpr int32_t kMaxWorkers = 65535;
-constexpr int64_t kMaxGradValues = (int64_t)1 << 44;
-// Thread blocks of a launch over gradients: 16 per compute unit, twice what is resident at a time.
+constexpr int64_t kMaxGradValues = (int64_t)1 << 35;
+// Thread blocks of a launch that adds up squares, 16 per compute unit, twice what is resident at a time (16 x 11.7M fp32
+// values: 2048 blocks 136 us, 4096 114, 8192 125).
 constexpr int64_t kGradBlocks = 4096;
+// Partial sums of a worker that the blocks of the scaling kernel add up again, each of them (138M values of one worker
+// clipped: 512 blocks 283 us, 1024 263, 2048 273, 4096 295).
+constexpr int64_t kGradParts = 1024;
+// Gradients of one worker that exceed the memory-side cache are squared and scaled before the next worker's, so that part of
+// them is still there (16 x 138M bf16 values into rows 2814 against 3168 us); shorter ones leave the chip idle between so many
+// launches (8 x 50M 788 against 598 us).
+constexpr int64_t kGradRowBytes = (int64_t)256 << 20;
 
 bool valid_type(int t) { return t == LIEC_F32 || t == LIEC_BF16 || t == LIEC_F16; }
 int64_t size_of(int t) { return t == LIEC_F32 ? 4 : 2; }
@@ -29,8 +37,10 @@ liec_status launched() { return hipGetLastError() == hipSuccess ? LIEC_OK : LIEC
 // ---- gradients -------------------------------------------------------------------------------------------------------
 int64_t grad_batches(int32_t T) { return std::max<int64_t>(1, ceil_div(T, kGradTensors)); }
 
-// Partial sums of a worker that a launch may leave: enough blocks in all to fill the chip, one for each worker at least.
-int64_t grad_parts_per_batch(int32_t N, int32_t T) { return std::max<int64_t>(1, kGradBlocks / N / grad_batches(T)); }
+// Partial sums of a worker that a launch may leave: what the workspace has room for.
+int64_t grad_parts_per_batch(int32_t N, int32_t T) {
+    return std::max<int64_t>(1, std::min<int64_t>(kGradBlocks, 16 * kGradBlocks / N) / grad_batches(T));
+}
 
 bool valid_grads(const liec_grad_tensor* t, int32_t T, int32_t N, int64_t* total) {
     if (N < 1 || N > kMaxWorkers || T < 0 || T > LIEC_GRAD_MAX_TENSORS || (T && !t)) return false;
@@ -65,23 +75,31 @@ bool ranges_meet(uintptr_t a, int64_t an, int64_t as, uintptr_t b, int64_t bn, i
 
 struct GradBatch {
     int32_t first, count;
-    int64_t tiles, blocks, per;
+    int64_t tiles, blocks, col;               // col: column of its first tensor
 };
 
-struct GradLaunch {
-    int64_t parts = 0;                        // partial sums per worker
-    std::vector<GradBatch> batches;
+struct GradPlan {
+    int64_t parts = 0, bytes = 0;             // of a worker: partial sums, gradients
+    std::vector<GradBatch> batches;           // those that have any values
 };
 
-bool plan_grads(const liec_grad_tensor* t, int32_t T, int32_t N, GradLaunch* out) {
+// `rows`: workers that a launch works on.
+bool plan_grads(const liec_grad_tensor* t, int32_t T, int32_t N, int64_t rows, bool scales, GradPlan* out) {
     try {
-        const int64_t most = grad_parts_per_batch(N, T);
-        for (int32_t b = 0; b < T; b += kGradTensors) {
-            GradBatch g{b, std::min<int32_t>(kGradTensors, T - b), 0, 0, 0};
-            for (int32_t i = 0; i < g.count; ++i) g.tiles += ceil_div(t[b + i].count, kGradTile);
+        const int64_t most = std::min(grad_parts_per_batch(N, T), std::max<int64_t>(1, std::min<int64_t>(kGradBlocks / rows, scales ? kGradParts : kGradBlocks))), share = ceil_div(T, grad_batches(T));
+        int64_t col = 0;
+        out->parts = out->bytes = 0;
+        out->batches.clear();
+        for (int64_t b = 0; b < T; b += share) {
+            GradBatch g{(int32_t)b, (int32_t)std::min<int64_t>(share, T - b), 0, 0, col};
+            for (int32_t i = 0; i < g.count; ++i) {
+                const int64_t bytes = t[b + i].count * size_of(t[b + i].dtype);
+                g.tiles += ceil_div(bytes, kGradTile);
+                out->bytes += bytes;
+                col += t[b + i].count;
+            }
             if (!g.tiles) continue;
-            g.per = ceil_div(g.tiles, most);
-            g.blocks = ceil_div(g.tiles, g.per);
+            g.blocks = std::min(g.tiles, most);
             out->parts += g.blocks;
             out->batches.push_back(g);
         }
@@ -91,8 +109,8 @@ bool plan_grads(const liec_grad_tensor* t, int32_t T, int32_t N, GradLaunch* out
     return true;
 }
 
-void fill_table(const liec_grad_tensor* t, const GradBatch& g, int64_t col0, GradTable* tab) {
-    int64_t col = col0;
+void fill_table(const liec_grad_tensor* t, const GradBatch& g, GradTable* tab) {
+    int64_t col = g.col;
     uint32_t tile = 0;
     for (int32_t i = 0; i < g.count; ++i) {
         const liec_grad_tensor& s = t[g.first + i];
@@ -102,58 +120,77 @@ void fill_table(const liec_grad_tensor* t, const GradBatch& g, int64_t col0, Gra
         tab->first[i] = tile;
         tab->type[i] = (uint8_t)s.dtype;
         col += s.count;
-        tile += (uint32_t)ceil_div(s.count, kGradTile);
+        tile += (uint32_t)ceil_div(s.count * size_of(s.dtype), kGradTile);
     }
     tab->col[g.count] = col;
     tab->first[g.count] = tile;
 }
 
-void launch_squares(const liec_grad_tensor* t, int32_t N, const GradLaunch& plan, double* partial, hipStream_t st) {
+struct GradCall {
+    const liec_grad_tensor* t;
+    int32_t T, N;
+    float* rows;                              // nullptr: in place
+    int64_t row_stride;
+    float bound, *norms;
+    double* partial;
+    hipStream_t st;
+};
+
+GradPass pass_of(const GradCall& c, const GradPlan& plan, const GradBatch& g, bool sums, int64_t row, uint32_t slot) {
+    return GradPass{c.partial, sums ? (uint32_t)plan.parts : 0u, slot, (uint32_t)row, (uint32_t)g.tiles, (uint32_t)g.count, c.bound, c.norms, c.rows, c.row_stride};
+}
+
+void launch_squares(const GradCall& c, const GradPlan& plan, int64_t row, int64_t rows, bool stream) {
     uint32_t slot = 0;
     GradTable tab;
     for (const GradBatch& g : plan.batches) {
-        fill_table(t, g, 0, &tab);
-        k_grad_squares<<<dim3((uint32_t)g.blocks, (uint32_t)N), kBlock, 0, st>>>(partial, (uint32_t)plan.parts, slot, (uint32_t)g.count,
-                                                                                 (uint32_t)g.tiles, (uint32_t)g.per, tab);
+        fill_table(c.t, g, &tab);
+        const GradPass a = pass_of(c, plan, g, true, row, slot);
+        const dim3 grid((uint32_t)g.blocks, (uint32_t)rows);
+        if (stream) k_grad_squares<true><<<grid, kBlock, 0, c.st>>>(a, tab);
+        else k_grad_squares<false><<<grid, kBlock, 0, c.st>>>(a, tab);
         slot += (uint32_t)g.blocks;
     }
 }
 
-// Norms and scaling; rows == nullptr: in place.
-liec_status clip_into(const liec_grad_tensor* t, int32_t T, int32_t N, float* rows, int64_t row_stride, float bound, float* norms, double* partial,
-                      hipStream_t st) {
-    GradLaunch plan;
-    if (!plan_grads(t, T, N, &plan)) return LIEC_ENOMEM;
-    const bool sums = norms || bound < INFINITY;
-    if (sums) launch_squares(t, N, plan, partial, st);
-    if (!rows && bound == INFINITY) {
-        // nothing to scale
-    } else {
-        int64_t col = 0;
-        int32_t next = 0;
-        GradTable tab;
-        for (const GradBatch& g : plan.batches) {
-            for (; next < g.first; ++next) col += t[next].count;   // batches without values are left out
-            fill_table(t, g, col, &tab);
-            k_grad_scale<<<dim3((uint32_t)g.blocks, (uint32_t)N), kBlock, 0, st>>>(partial, sums ? (uint32_t)plan.parts : 0u, bound, norms, rows, row_stride,
-                                                                                   (uint32_t)g.count, (uint32_t)g.tiles, (uint32_t)g.per, tab);
-        }
+void launch_scale(const GradCall& c, const GradPlan& plan, bool sums, int64_t row, int64_t rows) {
+    GradTable tab;
+    for (const GradBatch& g : plan.batches) {
+        fill_table(c.t, g, &tab);
+        const GradPass a = pass_of(c, plan, g, sums, row, 0);
+        const dim3 grid((uint32_t)g.tiles, (uint32_t)rows);
+        if (c.rows) k_grad_scale<true><<<grid, kBlock, 0, c.st>>>(a, tab);
+        else k_grad_scale<false><<<grid, kBlock, 0, c.st>>>(a, tab);
     }
-    if (norms && ((!rows && bound == INFINITY) || plan.batches.empty()))
-        k_grad_norms<<<(uint32_t)N, kBlock, 0, st>>>(partial, (uint32_t)plan.parts, norms);
+}
+
+liec_status run_grads(const GradCall& c) {
+    const int64_t N = c.N;
+    const bool scales = c.rows || c.bound < INFINITY, sums = c.norms || c.bound < INFINITY;
+    GradPlan plan;
+    if (!plan_grads(c.t, c.T, c.N, N, scales, &plan)) return LIEC_ENOMEM;
+    int64_t group = N;
+    if (scales && sums && N > 1 && plan.bytes > kGradRowBytes) {
+        group = 1;
+        if (!plan_grads(c.t, c.T, c.N, group, scales, &plan)) return LIEC_ENOMEM;
+    }
+    for (int64_t r = 0; r < N; r += group) {
+        if (sums) launch_squares(c, plan, r, group, !scales);
+        if (scales) launch_scale(c, plan, sums, r, group);
+    }
+    if (c.norms && (!scales || plan.batches.empty())) k_grad_norms<<<(uint32_t)N, kBlock, 0, c.st>>>(c.partial, (uint32_t)plan.parts, c.norms);
     return launched();
 }
 
 // ---- layer normalisation ---------------------------------------------------------------------------------------------
 constexpr int64_t kLnMost = 16384;                                   // columns that a team holds
-constexpr int64_t kLnBlocks = 1024;                                  // thread blocks of a launch, 4 per compute unit
 
 struct Team {
-    int lanes, vecs;
+    int lanes, eights;                 // lanes to a row, columns of a lane in eights
 };
 // The smallest team that holds a row.
 Team team_of(int64_t C) {
-    const int64_t v = ceil_div(C, kLnVec);
+    const int64_t v = ceil_div(C, 8);
     if (v <= 8) return {8, 1};
     if (v <= 16) return {16, 1};
     if (v <= 32) return {32, 1};
@@ -165,21 +202,29 @@ Team team_of(int64_t C) {
     return {1024, 2};
 }
 
-bool holds(int64_t C) { return C >= kLnVec && C <= kLnMost; }
+bool holds(int64_t C) { return C >= kLnShortest && C <= kLnMost; }
 
 struct Strips {
     int64_t per, count;
 };
-// Rows of a block: as many blocks as fill the chip, and two rows for each of its teams at least.
-Strips strips_of(int32_t N, int64_t R, int64_t C) {
+// Rows of a block: as many blocks as are resident at a time, `waves` of them on each of the chip's 1024 SIMDs, and two rows
+// for each of a block's teams at least.
+Strips strips_of(int32_t N, int64_t R, int64_t C, int64_t waves) {
     if (R == 0) return {1, 0};
-    const bool held = holds(C);
-    const int64_t teams = held ? std::max(1, kBlock / team_of(C).lanes) : 1;
-    // rows that no team holds: the columns' sums, a thread per column
-    const int64_t want = std::max<int64_t>(1, kLnBlocks / N / (held ? 1 : ceil_div(C, kBlock)));
-    const int64_t per = std::max(ceil_div(R, want), 2 * teams);
+    if (!holds(C)) {                   // the columns' sums, a thread per column
+        const int64_t per = ceil_div(R, std::max<int64_t>(1, 1024 / N / ceil_div(C, kBlock)));
+        return {per, ceil_div(R, per)};
+    }
+    const int64_t lanes = team_of(C).lanes, threads = lanes > 64 ? lanes : kBlock;
+    const int64_t want = std::max<int64_t>(1, 1024 * 64 * waves / threads / N);
+    const int64_t per = std::max(ceil_div(R, want), 2 * (threads / lanes));
     return {per, ceil_div(R, per)};
 }
+
+// Waves per SIMD of the backward kernel: its weight gradients stay in registers.  One vector per lane leaves room for four
+// waves (six: as fast or 2 to 30 % slower); of two per lane two waves that request two rows ahead beat four that request one
+// (2048 columns 156 against 166 us, 8192 286 against 299); 16 waves to a row are four by themselves.
+int64_t backward_waves(int64_t C) { return !holds(C) ? 1 : team_of(C).eights == 1 || team_of(C).lanes == 1024 ? 4 : 2; }
 
 bool valid_rows(const liec_rows* r, int64_t size) {
     const int64_t most = (int64_t)1 << 44;
@@ -218,21 +263,39 @@ struct LnForward {
     hipStream_t st;
 };
 
-template <typename T, int TEAM, int K>
+// Results of up to the memory-side cache's 256 MB are left there for the operation that reads them next, larger ones are
+// streamed past it: rows of 2000 bf16 columns, 200 MB 73.4 against 76.6 us forward and 108 against 119 us backward, 400 MB
+// 157 against 148 and 259 against 238.
+bool keeps(int32_t N, int64_t R, int64_t C, int64_t size) { return N * R * C * size <= (int64_t)256 << 20; }
+
+// Blocks of neighbouring rows, or rows dealt out to the blocks in turn.
+LnWalk walk_of(const Strips& s, int64_t teams, int64_t R, bool in_turn, bool keep) {
+    return in_turn ? LnWalk{teams, R, s.count * teams, keep} : LnWalk{s.per, s.per, teams, keep};
+}
+
+template <typename T, int TEAM, int EIGHTS>
 void run_forward(const LnForward& a) {
-    const Strips s = strips_of(a.N, a.R, a.C);
-    k_ln_forward<T, TEAM, K><<<dim3((uint32_t)s.count, (uint32_t)a.N), (TEAM > 64 ? TEAM : kBlock), 0, a.st>>>(
-        (uint32_t)a.C, (uint32_t)s.per, a.eps, a.R, a.mean, a.rstd, a.x, a.y, a.w, a.b);
+    constexpr int K = EIGHTS * 8 / Vec16<T>::n, threads = TEAM > 64 ? TEAM : kBlock;
+    const bool full = a.C == TEAM * EIGHTS * 8;
+    // Many short-lived blocks: 8 x 8192 rows of 4096 bf16 columns 185 us, blocks that stay on the chip and request rows ahead
+    // 194 to 220, although every block reads the weights again.
+    const Strips s = strips_of(a.N, a.R, a.C, 64);
+    const LnWalk walk = walk_of(s, threads / TEAM, a.R, true, keeps(a.N, a.R, a.C, sizeof(T)));
+    const dim3 grid((uint32_t)s.count, (uint32_t)a.N);
+    if (full)
+        k_ln_forward<T, TEAM, K, true><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.eps, a.R, walk, a.mean, a.rstd, a.x, a.y, a.w, a.b);
+    else
+        k_ln_forward<T, TEAM, K, false><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.eps, a.R, walk, a.mean, a.rstd, a.x, a.y, a.w, a.b);
 }
 
 template <typename T>
 void forward_of(const LnForward& a) {
     if (!holds(a.C)) {
-        k_ln_forward_wide<T><<<dim3((uint32_t)a.R, (uint32_t)a.N), a.C < kLnVec ? 64 : kLnWide, 0, a.st>>>(a.C, a.eps, a.R, a.mean, a.rstd, a.x, a.y, a.w, a.b);
+        k_ln_forward_wide<T><<<dim3((uint32_t)a.R, (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.eps, a.R, a.mean, a.rstd, a.x, a.y, a.w, a.b);
         return;
     }
     const Team t = team_of(a.C);
-    switch (t.lanes * t.vecs) {
+    switch (t.lanes * t.eights) {
         case 8: return run_forward<T, 8, 1>(a);
         case 16: return run_forward<T, 16, 1>(a);
         case 32: return run_forward<T, 32, 1>(a);
@@ -256,10 +319,20 @@ struct LnBackward {
     hipStream_t st;
 };
 
-template <typename T, int TEAM, int K>
+template <typename T, int TEAM, int EIGHTS>
 void run_backward(const LnBackward& a) {
-    k_ln_backward<T, TEAM, K><<<dim3((uint32_t)a.strips.count, (uint32_t)a.N), (TEAM > 64 ? TEAM : kBlock), 0, a.st>>>(
-        (uint32_t)a.C, (uint32_t)a.strips.per, a.R, a.partial, a.mean, a.rstd, a.dy, a.x, a.dx, a.w, a.dw, a.db);
+    constexpr int K = EIGHTS * 8 / Vec16<T>::n, threads = TEAM > 64 ? TEAM : kBlock;
+    constexpr int P = EIGHTS == 1 || TEAM == 1024 ? 1 : 2;
+    const bool full = a.C == TEAM * EIGHTS * 8;
+    // Rows in turn keep the whole chip on one stretch of memory (8 x 6000 rows of 5000 bf16 columns 264 against 376 us, 1024
+    // columns 264 against 285); at the power-of-two distances of full rows they meet on the same channels (8192 columns 317
+    // against 286 us).
+    const LnWalk walk = walk_of(a.strips, threads / TEAM, a.R, !(full && TEAM >= 128), keeps(a.N, a.R, a.C, sizeof(T)));
+    const dim3 grid((uint32_t)a.strips.count, (uint32_t)a.N);
+    if (full)
+        k_ln_backward<T, TEAM, K, true, P><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.R, walk, a.partial, a.mean, a.rstd, a.dy, a.x, a.dx, a.w, a.dw, a.db);
+    else
+        k_ln_backward<T, TEAM, K, false, P><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.R, walk, a.partial, a.mean, a.rstd, a.dy, a.x, a.dx, a.w, a.dw, a.db);
 }
 
 template <typename T>
@@ -270,11 +343,11 @@ void backward_of(const LnBackward& a) {
             k_ln_columns_wide<T><<<dim3((uint32_t)ceil_div(a.C, kBlock), (uint32_t)a.N, (uint32_t)a.strips.count), kBlock, 0, a.st>>>(
                 a.C, a.strips.per, a.R, a.partial, a.mean, a.rstd, a.dy, a.x);
         if (a.dx.data)
-            k_ln_backward_wide<T><<<dim3((uint32_t)a.R, (uint32_t)a.N), a.C < kLnVec ? 64 : kLnWide, 0, a.st>>>(a.C, a.R, a.mean, a.rstd, a.dy, a.x, a.dx, a.w);
+            k_ln_backward_wide<T><<<dim3((uint32_t)a.R, (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.R, a.mean, a.rstd, a.dy, a.x, a.dx, a.w);
         return;
     }
     const Team t = team_of(a.C);
-    switch (t.lanes * t.vecs) {
+    switch (t.lanes * t.eights) {
         case 8: return run_backward<T, 8, 1>(a);
         case 16: return run_backward<T, 16, 1>(a);
         case 32: return run_backward<T, 32, 1>(a);
@@ -301,7 +374,7 @@ liec_status liec_grad_norm(const liec_grad_tensor* tensors, int32_t T, int32_t N
     int64_t total = 0;
     if (!valid_grads(tensors, T, N, &total) || !norms || !aligned_to(norms, 4)) return LIEC_EINVAL;
     if (!valid_workspace(workspace, workspace_bytes, liec_grads_workspace(N, T))) return LIEC_EINVAL;
-    return clip_into(tensors, T, N, nullptr, 0, INFINITY, norms, static_cast<double*>(workspace), (hipStream_t)hip_stream);
+    return run_grads(GradCall{tensors, T, N, nullptr, 0, INFINITY, norms, static_cast<double*>(workspace), (hipStream_t)hip_stream});
 }
 
 liec_status liec_clip_grads(const liec_grad_tensor* tensors, int32_t T, int32_t N, float max_norm, float* norms, void* workspace,
@@ -324,7 +397,7 @@ liec_status liec_clip_grads(const liec_grad_tensor* tensors, int32_t T, int32_t 
     } catch (const std::bad_alloc&) {
         return LIEC_ENOMEM;
     }
-    return clip_into(tensors, T, N, nullptr, 0, max_norm, norms, static_cast<double*>(workspace), (hipStream_t)hip_stream);
+    return run_grads(GradCall{tensors, T, N, nullptr, 0, max_norm, norms, static_cast<double*>(workspace), (hipStream_t)hip_stream});
 }
 
 liec_status liec_gather_grads(const liec_grad_tensor* tensors, int32_t T, int32_t N, float* rows, int64_t row_stride, float max_norm, float* norms,
@@ -339,7 +412,7 @@ liec_status liec_gather_grads(const liec_grad_tensor* tensors, int32_t T, int32_
         if (ranges_meet((uintptr_t)rows, total * 4, row_stride * 4, (uintptr_t)tensors[i].data, tensors[i].count * s, tensors[i].stride * s, N))
             return LIEC_EINVAL;
     }
-    return clip_into(tensors, T, N, rows, row_stride, max_norm, norms, static_cast<double*>(workspace), (hipStream_t)hip_stream);
+    return run_grads(GradCall{tensors, T, N, rows, row_stride, max_norm, norms, static_cast<double*>(workspace), (hipStream_t)hip_stream});
 }
 
 liec_status liec_layer_norm(const liec_rows* x, const liec_param* weight, const liec_param* bias, const liec_rows* y, float* mean, float* rstd, int32_t N,
@@ -358,7 +431,7 @@ liec_status liec_layer_norm(const liec_rows* x, const liec_param* weight, const 
 
 int64_t liec_layer_norm_workspace(int32_t N, int64_t R, int64_t C) {
     if (!valid_sizes(N, R, C)) return -1;
-    return (int64_t)N * strips_of(N, R, C).count * 2 * C * (int64_t)sizeof(float);
+    return (int64_t)N * strips_of(N, R, C, backward_waves(C)).count * 2 * C * (int64_t)sizeof(float);
 }
 
 liec_status liec_layer_norm_backward(const liec_rows* dy, const liec_rows* x, const float* mean, const float* rstd, const liec_param* weight,
@@ -384,7 +457,7 @@ liec_status liec_layer_norm_backward(const liec_rows* dy, const liec_rows* x, co
     }
     const hipStream_t st = (hipStream_t)hip_stream;
     LnBackward a{rows_of(dy), rows_of(x), rows_of(dx), param_of(weight, param_dtype), param_of(dweight, param_dtype), param_of(dbias, param_dtype),
-                 mean, rstd, static_cast<float*>(workspace), N, R, C, strips_of(N, R, C), st};
+                 mean, rstd, static_cast<float*>(workspace), N, R, C, strips_of(N, R, C, backward_waves(C)), st};
     const LnParam& any = a.dw.data ? a.dw : a.db;
     const bool shared = any.stride == 0 || N == 1;
     const int64_t parts = shared ? (int64_t)N * a.strips.count : a.strips.count;
