@@ -28,12 +28,6 @@ struct LnParam {                       // a [workers, columns] tensor of unit co
     uint32_t type;
 };
 
-// Rows of a thread block: from blockIdx.x * pitch on, at most `span` of them, a team's own at distances of `step`.
-struct LnWalk {
-    int64_t pitch, span, step;
-    bool keep;                         // results are left in the caches for whoever reads them next
-};
-
 // ---- sums over a team --------------------------------------------------------------------------------------------
 template <int CTRL>
 __device__ __forceinline__ float dpp_move(float v) {
@@ -110,15 +104,16 @@ __device__ __forceinline__ void load_param(const LnParam& p, uint32_t worker, ui
 }
 
 // ---- forward -------------------------------------------------------------------------------------------------------
-// Block (strip, worker): rows strip * per .. of the worker, TEAM lanes to a row, the next row of a team requested ahead.
+// Block (b, worker): TEAM lanes to a row, rows dealt out to the blocks' teams in turn, the next row of a team requested ahead.
+// keep: the results are left in the caches for whoever reads them next.
 template <typename T, int TEAM, int K, bool FULL>
-__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_forward(uint32_t C, float eps, int64_t R, LnWalk walk, float* __restrict__ mean,
+__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_forward(uint32_t C, float eps, int64_t R, bool keep, float* __restrict__ mean,
                                                                             float* __restrict__ rstd, LnRows x, LnRows y, LnParam w, LnParam b) {
-    constexpr int WAVES = TEAM > 64 ? TEAM / 64 : 1, V = Vec16<T>::n;
+    constexpr int TEAMS = TEAM > 64 ? 1 : kBlock / TEAM, WAVES = TEAM > 64 ? TEAM / 64 : 1, V = Vec16<T>::n;
     constexpr int LANES = TEAM > 64 ? 64 : TEAM;
     __shared__ float lds[2][2][WAVES];
     const uint32_t worker = blockIdx.y, l = threadIdx.x % TEAM, team = team_index<TEAM>(), wave = l >> 6;
-    const int64_t begin = (int64_t)blockIdx.x * walk.pitch, first = begin + team, end = min(begin + walk.span, R), step = walk.step;
+    const int64_t first = (int64_t)blockIdx.x * TEAMS + team, step = (int64_t)gridDim.x * TEAMS;
     const T* const xs = static_cast<const T*>(x.data) + (int64_t)worker * x.worker;
     T* const ys = static_cast<T*>(y.data) + (int64_t)worker * y.worker;
     const int64_t stat = (int64_t)worker * R;
@@ -126,7 +121,7 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_forward(uint
 #pragma unroll
     for (int k = 0; k < K; ++k) at[k] = vec_start<TEAM, V, FULL>(l, k, C, skip[k]);
     v4u held[K];
-    if (first < end) {
+    if (first < R) {
 #pragma unroll
         for (int k = 0; k < K; ++k) held[k] = ld16<T, true>(in_row(xs + first * x.row, at[k]));
     }
@@ -152,11 +147,11 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_forward(uint
         others_inv = 1.f / fmaxf(others, 1.f);
     }
     uint32_t parity = 0;
-    for (int64_t r = first; r < end; r += step) {
+    for (int64_t r = first; r < R; r += step) {
         float f[K][V];
 #pragma unroll
         for (int k = 0; k < K; ++k) Vec16<T>::widen(held[k], f[k]);
-        if (r + step < end) {
+        if (r + step < R) {
 #pragma unroll
             for (int k = 0; k < K; ++k) held[k] = ld16<T, true>(in_row(xs + (r + step) * x.row, at[k]));
         }
@@ -195,7 +190,7 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_forward(uint
             float o[V];
 #pragma unroll
             for (int j = 0; j < V; ++j) o[j] = __fmaf_rn((f[k][j] - mu) * rs, wv[k][j], bv[k][j]);
-            if (!may_end<TEAM, K, FULL>(k) || skip[k] < V) st16_as<T>(walk.keep, in_row(ys + r * y.row, at[k]), Vec16<T>::narrow(o));
+            if (!may_end<TEAM, K, FULL>(k) || skip[k] < V) st16_as<T>(keep, in_row(ys + r * y.row, at[k]), Vec16<T>::narrow(o));
         }
         if (l == 0) {
             if (mean) mean[stat + r] = mu;
@@ -241,19 +236,19 @@ __global__ __launch_bounds__(kLnWide) void k_ln_forward_wide(int64_t C, float ep
 }
 
 // ---- backward ------------------------------------------------------------------------------------------------------
-// Block (strip, worker): dx of its rows, and their share of dw and db in registers, which it leaves in partial[worker][strip]
+// Block (b, worker): dx of its rows, and their share of dw and db in registers, which it leaves in partial[worker][b]
 // (2 x C values), or in dw and db themselves where it is the only one (partial == nullptr).  The next P rows of a
 // team are requested ahead.
 template <typename T, int TEAM, int K, bool FULL, int P>
-__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock), (K * Vec16<T>::n == 8 || TEAM == 1024 ? 4 : 2)) void k_ln_backward(uint32_t C, int64_t R, LnWalk walk, float* __restrict__ partial,
+__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock), (K * Vec16<T>::n == 8 || TEAM == 1024 ? 4 : 2)) void k_ln_backward(uint32_t C, int64_t R, bool keep, float* __restrict__ partial,
                                                                                 const float* __restrict__ mean, const float* __restrict__ rstd, LnRows dy,
                                                                                 LnRows x, LnRows dx, LnParam w, LnParam dw, LnParam db) {
-    constexpr int WAVES = TEAM > 64 ? TEAM / 64 : 1, V = Vec16<T>::n;
+    constexpr int TEAMS = TEAM > 64 ? 1 : kBlock / TEAM, WAVES = TEAM > 64 ? TEAM / 64 : 1, V = Vec16<T>::n;
     constexpr int LANES = TEAM > 64 ? 64 : TEAM, COLS = TEAM <= 64 ? TEAM * K * V : 1;
     __shared__ float lds[2][2][WAVES];
     __shared__ __align__(16) float sums[2][COLS];
     const uint32_t worker = blockIdx.y, l = threadIdx.x % TEAM, team = team_index<TEAM>();
-    const int64_t begin = (int64_t)blockIdx.x * walk.pitch, first = begin + team, end = min(begin + walk.span, R), step = walk.step;
+    const int64_t first = (int64_t)blockIdx.x * TEAMS + team, step = (int64_t)gridDim.x * TEAMS;
     const T* const xs = static_cast<const T*>(x.data) + (int64_t)worker * x.worker;
     const T* const gs = static_cast<const T*>(dy.data) + (int64_t)worker * dy.worker;
     T* const os = static_cast<T*>(dx.data) + (int64_t)worker * dx.worker;
@@ -265,18 +260,22 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock), (K * Vec16<T>::n == 8 
     for (int k = 0; k < K; ++k) at[k] = vec_start<TEAM, V, FULL>(l, k, C, skip[k]);
     v4u rx[P][K], rg[P][K];
     float mu[P], rs[P];
+    // 0, in a vector register: mean and rstd come with the row's vectors.  As scalar loads they were waited for at the next LDS
+    // access (8 x 8192 rows of 4096 bf16 columns 296 -> 279 us).
+    uint32_t none;
+    asm volatile("v_mov_b32 %0, 0" : "=v"(none));
     auto request = [&](int64_t r, v4u (&vx)[K], v4u (&vg)[K], float& m, float& s) {
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             vx[k] = ld16<T, true>(in_row(xs + r * x.row, at[k]));
             vg[k] = ld16<T, true>(in_row(gs + r * dy.row, at[k]));
         }
-        m = mus[r];
-        s = rss[r];
+        m = mus[r + none];
+        s = rss[r + none];
     };
 #pragma unroll
     for (int q = 0; q < P; ++q)
-        if (first + q * step < end) request(first + q * step, rx[q], rg[q], mu[q], rs[q]);
+        if (first + q * step < R) request(first + q * step, rx[q], rg[q], mu[q], rs[q]);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         load_param<V>(w, worker, at[k], 1.f, wv[k]);
@@ -304,7 +303,7 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock), (K * Vec16<T>::n == 8 
             }
         }
         const float rs_now = s;
-        if (r + P * step < end) request(r + P * step, vx, vg, m, s);
+        if (r + P * step < R) request(r + P * step, vx, vg, m, s);
         s1 = lanes_sum<LANES>(s1);
         s2 = lanes_sum<LANES>(s2);
         if (WAVES > 1) {
@@ -324,14 +323,14 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock), (K * Vec16<T>::n == 8 
                 float o[V];
 #pragma unroll
                 for (int j = 0; j < V; ++j) o[j] = rs_now * __fmaf_rn(-h[k][j], c2, a[k][j] - c1);
-                if (!may_end<TEAM, K, FULL>(k) || skip[k] < V) st16_as<T>(walk.keep, in_row(os + r * dx.row, at[k]), Vec16<T>::narrow(o));
+                if (!may_end<TEAM, K, FULL>(k) || skip[k] < V) st16_as<T>(keep, in_row(os + r * dx.row, at[k]), Vec16<T>::narrow(o));
             }
         }
     };
-    for (int64_t r = first; r < end; r += P * step) {
+    for (int64_t r = first; r < R; r += P * step) {
 #pragma unroll
         for (int q = 0; q < P; ++q)
-            if (r + q * step < end) row(r + q * step, rx[q], rg[q], mu[q], rs[q]);
+            if (r + q * step < R) row(r + q * step, rx[q], rg[q], mu[q], rs[q]);
     }
     if (!dw.data && !db.data) return;
     float* const out = partial ? partial + ((size_t)worker * gridDim.x + blockIdx.x) * 2 * C : nullptr;

@@ -202,6 +202,9 @@ Team team_of(int64_t C) {
     return {1024, 2};
 }
 
+int64_t threads_of(const Team& t) { return t.lanes > 64 ? t.lanes : kBlock; }
+int64_t teams_of(const Team& t) { return threads_of(t) / t.lanes; }
+
 bool holds(int64_t C) { return C >= kLnShortest && C <= kLnMost; }
 
 struct Strips {
@@ -215,9 +218,9 @@ Strips strips_of(int32_t N, int64_t R, int64_t C, int64_t waves) {
         const int64_t per = ceil_div(R, std::max<int64_t>(1, 1024 / N / ceil_div(C, kBlock)));
         return {per, ceil_div(R, per)};
     }
-    const int64_t lanes = team_of(C).lanes, threads = lanes > 64 ? lanes : kBlock;
-    const int64_t want = std::max<int64_t>(1, 1024 * 64 * waves / threads / N);
-    const int64_t per = std::max(ceil_div(R, want), 2 * (threads / lanes));
+    const Team t = team_of(C);
+    const int64_t want = std::max<int64_t>(1, 1024 * 64 * waves / threads_of(t) / N);
+    const int64_t per = std::max(ceil_div(R, want), 2 * teams_of(t));
     return {per, ceil_div(R, per)};
 }
 
@@ -225,6 +228,12 @@ Strips strips_of(int32_t N, int64_t R, int64_t C, int64_t waves) {
 // waves (six: as fast or 2 to 30 % slower); of two per lane two waves that request two rows ahead beat four that request one
 // (2048 columns 156 against 166 us, 8192 286 against 299); 16 waves to a row are four by themselves.
 int64_t backward_waves(int64_t C) { return !holds(C) ? 1 : team_of(C).eights == 1 || team_of(C).lanes == 1024 ? 4 : 2; }
+
+// Strips of the backward kernel.  Up to 8 rows for each of a block's teams stay in one block, whose sums need no second kernel.
+Strips backward_strips(int32_t N, int64_t R, int64_t C) {
+    if (holds(C) && R > 0 && R <= 8 * teams_of(team_of(C))) return {R, 1};
+    return strips_of(N, R, C, backward_waves(C));
+}
 
 bool valid_rows(const liec_rows* r, int64_t size) {
     const int64_t most = (int64_t)1 << 44;
@@ -268,11 +277,6 @@ struct LnForward {
 // 157 against 148 and 259 against 238.
 bool keeps(int32_t N, int64_t R, int64_t C, int64_t size) { return N * R * C * size <= (int64_t)256 << 20; }
 
-// Blocks of neighbouring rows, or rows dealt out to the blocks in turn.
-LnWalk walk_of(const Strips& s, int64_t teams, int64_t R, bool in_turn, bool keep) {
-    return in_turn ? LnWalk{teams, R, s.count * teams, keep} : LnWalk{s.per, s.per, teams, keep};
-}
-
 template <typename T, int TEAM, int EIGHTS>
 void run_forward(const LnForward& a) {
     constexpr int K = EIGHTS * 8 / Vec16<T>::n, threads = TEAM > 64 ? TEAM : kBlock;
@@ -280,12 +284,12 @@ void run_forward(const LnForward& a) {
     // Many short-lived blocks: 8 x 8192 rows of 4096 bf16 columns 185 us, blocks that stay on the chip and request rows ahead
     // 194 to 220, although every block reads the weights again.
     const Strips s = strips_of(a.N, a.R, a.C, 64);
-    const LnWalk walk = walk_of(s, threads / TEAM, a.R, true, keeps(a.N, a.R, a.C, sizeof(T)));
+    const bool keep = keeps(a.N, a.R, a.C, sizeof(T));
     const dim3 grid((uint32_t)s.count, (uint32_t)a.N);
     if (full)
-        k_ln_forward<T, TEAM, K, true><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.eps, a.R, walk, a.mean, a.rstd, a.x, a.y, a.w, a.b);
+        k_ln_forward<T, TEAM, K, true><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.eps, a.R, keep, a.mean, a.rstd, a.x, a.y, a.w, a.b);
     else
-        k_ln_forward<T, TEAM, K, false><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.eps, a.R, walk, a.mean, a.rstd, a.x, a.y, a.w, a.b);
+        k_ln_forward<T, TEAM, K, false><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.eps, a.R, keep, a.mean, a.rstd, a.x, a.y, a.w, a.b);
 }
 
 template <typename T>
@@ -322,17 +326,17 @@ struct LnBackward {
 template <typename T, int TEAM, int EIGHTS>
 void run_backward(const LnBackward& a) {
     constexpr int K = EIGHTS * 8 / Vec16<T>::n, threads = TEAM > 64 ? TEAM : kBlock;
-    constexpr int P = EIGHTS == 1 || TEAM == 1024 ? 1 : 2;
+    // Rows requested ahead: what registers allow.  Of 16-bit rows of 4096 columns three (two: 279.5 against 273 us for 8 x 8192
+    // rows, 287 against 275 for 4000 columns), of others two (5000 bf16 columns 266 against 334 us, 1000 fp32 columns 296
+    // against 322).
+    constexpr int P = EIGHTS == 1 || TEAM == 1024 ? 1 : TEAM == 256 && sizeof(T) == 2 ? 3 : 2;
     const bool full = a.C == TEAM * EIGHTS * 8;
-    // Rows in turn keep the whole chip on one stretch of memory (8 x 6000 rows of 5000 bf16 columns 264 against 376 us, 1024
-    // columns 264 against 285); at the power-of-two distances of full rows they meet on the same channels (8192 columns 317
-    // against 286 us).
-    const LnWalk walk = walk_of(a.strips, threads / TEAM, a.R, !(full && TEAM >= 128), keeps(a.N, a.R, a.C, sizeof(T)));
+    const bool keep = keeps(a.N, a.R, a.C, sizeof(T));
     const dim3 grid((uint32_t)a.strips.count, (uint32_t)a.N);
     if (full)
-        k_ln_backward<T, TEAM, K, true, P><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.R, walk, a.partial, a.mean, a.rstd, a.dy, a.x, a.dx, a.w, a.dw, a.db);
+        k_ln_backward<T, TEAM, K, true, P><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.R, keep, a.partial, a.mean, a.rstd, a.dy, a.x, a.dx, a.w, a.dw, a.db);
     else
-        k_ln_backward<T, TEAM, K, false, P><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.R, walk, a.partial, a.mean, a.rstd, a.dy, a.x, a.dx, a.w, a.dw, a.db);
+        k_ln_backward<T, TEAM, K, false, P><<<grid, threads, 0, a.st>>>((uint32_t)a.C, a.R, keep, a.partial, a.mean, a.rstd, a.dy, a.x, a.dx, a.w, a.dw, a.db);
 }
 
 template <typename T>
@@ -431,7 +435,7 @@ liec_status liec_layer_norm(const liec_rows* x, const liec_param* weight, const 
 
 int64_t liec_layer_norm_workspace(int32_t N, int64_t R, int64_t C) {
     if (!valid_sizes(N, R, C)) return -1;
-    return (int64_t)N * strips_of(N, R, C, backward_waves(C)).count * 2 * C * (int64_t)sizeof(float);
+    return (int64_t)N * backward_strips(N, R, C).count * 2 * C * (int64_t)sizeof(float);
 }
 
 liec_status liec_layer_norm_backward(const liec_rows* dy, const liec_rows* x, const float* mean, const float* rstd, const liec_param* weight,
@@ -457,7 +461,7 @@ liec_status liec_layer_norm_backward(const liec_rows* dy, const liec_rows* x, co
     }
     const hipStream_t st = (hipStream_t)hip_stream;
     LnBackward a{rows_of(dy), rows_of(x), rows_of(dx), param_of(weight, param_dtype), param_of(dweight, param_dtype), param_of(dbias, param_dtype),
-                 mean, rstd, static_cast<float*>(workspace), N, R, C, strips_of(N, R, C, backward_waves(C)), st};
+                 mean, rstd, static_cast<float*>(workspace), N, R, C, backward_strips(N, R, C), st};
     const LnParam& any = a.dw.data ? a.dw : a.db;
     const bool shared = any.stride == 0 || N == 1;
     const int64_t parts = shared ? (int64_t)N * a.strips.count : a.strips.count;

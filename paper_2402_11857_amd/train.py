@@ -9,6 +9,8 @@ from __future__ import annotations
 import ctypes
 import math
 from array import array
+from itertools import repeat
+from operator import attrgetter, floordiv
 from typing import Optional, Sequence, Tuple
 
 import torch
@@ -17,65 +19,86 @@ from .binding import _check, lib
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _dtype_code = _DTYPES.get
+_dtype_of = attrgetter("dtype")
+_Tensor = torch.Tensor
 
 
 def _stream(device: int) -> int:
     return torch.cuda.current_stream(device).cuda_stream
 
 
-def _on(device: int):
-    """The device of the tensors is the current one while a function launches."""
-    return torch.cuda.device(device)
+# the same without an object for the stream (1 us of a call), where torch has it
+_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream)
+
+
+def _call(name: str, device: int, *args) -> None:
+    """The entry point `name` on the current stream of `device`, which is the current device while it launches."""
+    function = getattr(lib(), name)
+    if torch.cuda.current_device() == device:
+        status = function(*args, _stream(device))
+    else:
+        with torch.cuda.device(device):
+            status = function(*args, _stream(device))
+    if status:
+        _check(status, name)
 
 
 # ---- gradients ------------------------------------------------------------------------------------------------------
-def _grad_table(grads: Sequence[torch.Tensor], N: int, whole: bool, device: int) -> array:
-    """liec_grad_tensor of each tensor, as the words the struct is made of."""
-    words = []
-    add = words.extend
-    for t in grads:
-        code = _dtype_code(t.dtype)
-        if code is None or t.get_device() != device:
-            raise TypeError("gradients must be float32, bfloat16 or float16 tensors on one GPU")
-        count = t.numel()
-        if whole:
-            if not t.is_contiguous():
-                raise ValueError("gradients of one worker must be contiguous")
-            add((t.data_ptr(), count, count, code))
-            continue
-        if t.dim() == 0 or t.shape[0] != N:
-            raise ValueError(f"a gradient has shape {tuple(t.shape)}, expected {N} workers as its leading dimension")
-        count //= N
-        if t.is_contiguous():
-            add((t.data_ptr(), count, count, code))
-        else:
-            if not t[0].is_contiguous():
+def _grad_table(grads: Sequence[torch.Tensor], N: int, whole: bool, device: int) -> Tuple[array, int]:
+    """(liec_grad_tensor of each tensor, as the words the struct is made of; values of a worker in all)"""
+    types = set(map(_dtype_of, grads))
+    if not types <= _DTYPES.keys() or not set(map(_Tensor.get_device, grads)) <= {device}:
+        raise TypeError("gradients must be float32, bfloat16 or float16 tensors on one GPU")
+    counts = list(map(_Tensor.numel, grads))
+    contiguous = all(map(_Tensor.is_contiguous, grads))
+    strides = counts
+    if whole:
+        if not contiguous:
+            raise ValueError("gradients of one worker must be contiguous")
+    else:
+        try:
+            leading = set(map(_Tensor.size, grads, repeat(0)))
+        except IndexError:                                     # a tensor without dimensions
+            leading = {None}
+        if not leading <= {N}:
+            raise ValueError(f"every gradient needs {N} workers as its leading dimension: {[tuple(t.shape) for t in grads][:8]}")
+        counts = strides = list(map(floordiv, counts, repeat(N)))
+        if not contiguous:
+            if not all(t[0].is_contiguous() for t in grads):
                 raise ValueError("the gradients of a worker must be contiguous within each tensor")
-            add((t.data_ptr(), count, t.stride(0), code))
-    return array("q", words)
+            strides = [n if t.is_contiguous() else t.stride(0) for t, n in zip(grads, counts)]
+    table = array("q", bytes(32 * len(counts)))
+    table[0::4] = array("q", map(_Tensor.data_ptr, grads))
+    table[1::4] = array("q", counts)
+    table[2::4] = array("q", strides)
+    if types != {torch.float32}:                               # whose code is 0
+        table[3::4] = array("q", map(_dtype_code, map(_dtype_of, grads)))
+    return table, sum(counts)
 
 
 def _grad_args(grads, norms, workers):
-    """(tensors' table, its length, N, device, workspace, its bytes)"""
-    if not grads and norms is None:
+    """(tensors' table, values of a worker, N, device, workspace, its bytes)"""
+    if norms is None and not grads:
         raise ValueError("no gradients, and no norms to tell the number of workers")
     first = grads[0] if grads else norms
     device = first.get_device()
     if device < 0:
         raise TypeError("gradients must be on the GPU")
+    if workers is not None and workers != 1:
+        raise ValueError("workers is 1 for tensors of one worker, or None for tensors with a leading dimension of workers")
+    N = 1 if workers else norms.numel() if norms is not None else first.shape[0] if first.dim() else 0
     if norms is not None:
         if norms.dtype != torch.float32 or norms.get_device() != device or norms.dim() != 1 or not norms.is_contiguous():
             raise TypeError("norms must be a contiguous float32 vector on the gradients' GPU")
-    if workers is not None and workers != 1:
-        raise ValueError("workers is 1 for tensors of one worker, or None for tensors with a leading dimension of workers")
-    N = 1 if workers == 1 else norms.shape[0] if norms is not None else first.shape[0] if first.dim() else 0
-    if norms is not None and norms.shape[0] != N:
-        raise ValueError(f"norms has {norms.shape[0]} values, expected {N}")
-    table = _grad_table(grads, N, workers == 1, device)
-    need = int(lib().liec_grads_workspace(N, len(grads)))
+        if norms.numel() != N:
+            raise ValueError(f"norms has {norms.numel()} values, expected {N}")
+    if N < 1:
+        raise ValueError("no workers")
+    table, total = _grad_table(grads, N, workers == 1, device)
+    need = lib().liec_grads_workspace(N, len(grads))
     if need < 0:
         raise ValueError(f"{len(grads)} tensors of {N} workers are more than the library takes")
-    return table, len(grads), N, device, torch.empty(need, dtype=torch.uint8, device=first.device), need
+    return table, total, N, device, torch.empty(need, dtype=torch.uint8, device=first.device), need
 
 
 def _optional(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -85,41 +108,38 @@ def _optional(t: Optional[torch.Tensor]) -> Optional[int]:
 def liec_grad_norm(grads: Sequence[torch.Tensor], norms: Optional[torch.Tensor] = None, workers: Optional[int] = None) -> torch.Tensor:
     """Global l2 norm of each worker's gradients over all tensors, [N] float32, summed in 64 bits.  `workers=1`: the
     tensors, of any shape, belong to one worker; otherwise their leading dimension is the workers'."""
-    table, T, N, device, ws, need = _grad_args(grads, norms, workers)
+    table, _, N, device, ws, need = _grad_args(grads, norms, workers)
     if norms is None:
-        norms = torch.empty(N, dtype=torch.float32, device=grads[0].device)
-    with _on(device):
-        _check(lib().liec_grad_norm(table.buffer_info()[0], T, N, norms.data_ptr(), ws.data_ptr(), need, _stream(device)), "liec_grad_norm")
+        norms = torch.empty(N, dtype=torch.float32, device=ws.device)
+    _call("liec_grad_norm", device, table.buffer_info()[0], len(grads), N, norms.data_ptr(), ws.data_ptr(), need)
     return norms
 
 
 def liec_clip_grads(grads: Sequence[torch.Tensor], max_norm: float, norms: Optional[torch.Tensor] = None, workers: Optional[int] = None) -> None:
     """Scales each worker's gradients in place so that their global norm is at most max_norm; `norms`, when given,
     receives the norms before that."""
-    table, T, N, device, ws, need = _grad_args(grads, norms, workers)
-    with _on(device):
-        _check(lib().liec_clip_grads(table.buffer_info()[0], T, N, max_norm, _optional(norms), ws.data_ptr(), need, _stream(device)),
-               "liec_clip_grads")
+    table, _, N, device, ws, need = _grad_args(grads, norms, workers)
+    _call("liec_clip_grads", device, table.buffer_info()[0], len(grads), N, max_norm, _optional(norms), ws.data_ptr(), need)
 
 
 def liec_gather_grads(grads: Sequence[torch.Tensor], rows: torch.Tensor, max_norm: float = math.inf, norms: Optional[torch.Tensor] = None,
                       workers: Optional[int] = None) -> None:
     """Puts each worker's tensors one after the other into its row of `rows` ([N, d] float32, as LiecContext.step reads
     it), scaled so that the row's norm is at most max_norm."""
-    table, T, N, device, ws, need = _grad_args(grads, norms, workers)
-    total = sum(table[1::4])
-    if rows.dtype != torch.float32 or rows.get_device() != device or rows.dim() != 2 or (rows.shape[1] > 1 and rows.stride(1) != 1):
+    table, total, N, device, ws, need = _grad_args(grads, norms, workers)
+    if rows.dtype != torch.float32 or rows.get_device() != device or rows.dim() != 2 or (rows.stride(1) != 1 and rows.shape[1] > 1):
         raise TypeError("rows must be a float32 [N, d] tensor on the gradients' GPU whose rows are contiguous")
     if rows.shape[0] != N or rows.shape[1] != total:
         raise ValueError(f"rows has shape {tuple(rows.shape)}, expected {(N, total)}")
-    with _on(device):
-        _check(lib().liec_gather_grads(table.buffer_info()[0], T, N, rows.data_ptr(), rows.stride(0), max_norm, _optional(norms), ws.data_ptr(),
-                                       need, _stream(device)), "liec_gather_grads")
+    _call("liec_gather_grads", device, table.buffer_info()[0], len(grads), N, rows.data_ptr(), rows.stride(0), max_norm, _optional(norms), ws.data_ptr(), need)
 
 
 # ---- layer normalisation --------------------------------------------------------------------------------------------
 class _Rows(ctypes.Structure):
     _fields_ = [("data", ctypes.c_void_p), ("worker_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+_ref = ctypes.byref
 
 
 class _Param(ctypes.Structure):
@@ -128,59 +148,65 @@ class _Param(ctypes.Structure):
 
 def _workers_of(x: torch.Tensor, params) -> Tuple[int, int, int]:
     """(N, R, C) of activations x under these weights, biases and their gradients (some of them None)."""
-    if x.dim() == 0 or x.shape[-1] < 1:
-        raise ValueError(f"activations of shape {tuple(x.shape)} have no columns")
-    C = x.shape[-1]
-    per_worker = 0
+    shape = x.shape
+    C = shape[-1] if shape else 0
+    if C < 1:
+        raise ValueError(f"activations of shape {tuple(shape)} have no columns")
+    N = 0
     for p in params:
         if p is None:
             continue
-        if p.dim() not in (1, 2) or p.shape[-1] != C or (C > 1 and p.stride(-1) != 1):
+        dims = p.dim()
+        if dims not in (1, 2) or p.size(-1) != C or (p.stride(-1) != 1 and C > 1):
             raise ValueError(f"a weight or bias of shape {tuple(p.shape)} does not fit {C} columns, or its columns are not contiguous")
-        if p.dim() == 2:
-            if x.dim() < 2 or p.shape[0] != x.shape[0] or not p.shape[0]:
-                raise ValueError(f"weights of {p.shape[0]} workers do not fit activations of shape {tuple(x.shape)}")
-            per_worker = p.shape[0]
-    if per_worker:
-        return per_worker, x.numel() // (per_worker * C), C
-    if x.dim() == 3 and not x.is_contiguous() and x.shape[0]:
-        return x.shape[0], x.shape[1], C
+        if dims == 2:
+            N = p.size(0)
+            if len(shape) < 2 or N != shape[0] or not N:
+                raise ValueError(f"weights of {N} workers do not fit activations of shape {tuple(shape)}")
+    if N:
+        return N, x.numel() // (N * C), C
+    if len(shape) == 3 and shape[0] and not x.is_contiguous():
+        return shape[0], shape[1], C
     return 1, x.numel() // C, C
 
 
-def _rows(t: torch.Tensor, N: int, R: int, C: int, like: torch.Tensor, what: str) -> _Rows:
-    if t.dtype != like.dtype or t.get_device() != like.get_device():
-        raise TypeError(f"{what} must have the activations' type and device")
-    if t.shape != like.shape:
-        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(like.shape)}")
+def _rows(t: torch.Tensor, N: int, R: int, C: int, what: str):
+    """liec_rows of a tensor that is N workers' R rows of C columns."""
     if t.is_contiguous():
-        return _Rows(t.data_ptr(), R * C, C)
+        return _ref(_Rows(t.data_ptr(), R * C, C))
     try:
         v = t.view(N, R, C)
     except RuntimeError:
         raise ValueError(f"{what} of strides {t.stride()} is not {N} workers' rows at equal distances") from None
     if C > 1 and v.stride(2) != 1:
         raise ValueError(f"the columns of {what} must be contiguous")
-    return _Rows(t.data_ptr(), v.stride(0), v.stride(1))
+    return _ref(_Rows(t.data_ptr(), v.stride(0), v.stride(1)))
 
 
-def _param(p: Optional[torch.Tensor], like: Optional[torch.Tensor], x: torch.Tensor) -> Optional[_Param]:
+def _like(t: torch.Tensor, x: torch.Tensor, what: str) -> None:
+    if t.dtype != x.dtype or t.get_device() != x.get_device():
+        raise TypeError(f"{what} must have the activations' type and device")
+    if t.shape != x.shape:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(x.shape)}")
+
+
+def _param(p: Optional[torch.Tensor], dtype, device: int):
     if p is None:
         return None
-    if p.get_device() != x.get_device() or p.dtype != like.dtype or _dtype_code(p.dtype) is None:
-        raise TypeError("weights, biases and their gradients must be float32, bfloat16 or float16, of one type, on the activations' GPU")
-    return _Param(p.data_ptr(), p.stride(0) if p.dim() == 2 else 0)
+    if p.dtype != dtype or p.get_device() != device:
+        raise TypeError("weights, biases and their gradients must be of one type, float32, bfloat16 or float16, on the activations' GPU")
+    return _ref(_Param(p.data_ptr(), p.stride(0) if p.dim() == 2 else 0))
 
 
-def _ref(s):
-    return None if s is None else ctypes.byref(s)
-
-
-def _activations_type(x: torch.Tensor) -> int:
-    code = _dtype_code(x.dtype)
-    if code is None or not x.is_cuda:
-        raise TypeError("activations must be float32, bfloat16 or float16 on the GPU")
-    return code
+def _param_type(*params):
+    """(type, its code) of the first one that is there."""
+    for p in params:
+        if p is not None:
+            code = _dtype_code(p.dtype)
+            if code is None:
+                raise TypeError("weights, biases and their gradients must be float32, bfloat16 or float16")
+            return p.dtype, code
+    return None, 0
 
 
 def liec_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5,
@@ -188,20 +214,21 @@ def liec_layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias
     """Layer normalisation over the last dimension: (y, mean, rstd), the latter two float32 of x's other dimensions.
     weight and bias: [C], or [N, C] for the N workers of x's leading dimension (columns of a models tensor, say).
     `out` may be x."""
-    code = _activations_type(x)
+    code, device = _dtype_code(x.dtype), x.get_device()
+    if code is None or device < 0:
+        raise TypeError("activations must be float32, bfloat16 or float16 on the GPU")
     N, R, C = _workers_of(x, (weight, bias))
-    like = weight if weight is not None else bias
-    w, b = _param(weight, like, x), _param(bias, like, x)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
-    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    xr = _rows(x, N, R, C, x, "x")
-    yr = _rows(y, N, R, C, x, "out")
-    device = x.get_device()
-    with _on(device):
-        _check(lib().liec_layer_norm(ctypes.byref(xr), _ref(w), _ref(b), ctypes.byref(yr), mean.data_ptr(), rstd.data_ptr(), N, R, C, eps, code,
-                                     0 if like is None else _DTYPES[like.dtype], _stream(device)), "liec_layer_norm")
-    return y, mean, rstd
+    ptype, pcode = _param_type(weight, bias)
+    w, b = _param(weight, ptype, device), _param(bias, ptype, device)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _like(out, x, "out")
+    lead = x.shape[:-1]
+    mean = torch.empty(lead, dtype=torch.float32, device=x.device)
+    rstd = torch.empty(lead, dtype=torch.float32, device=x.device)
+    _call("liec_layer_norm", device, _rows(x, N, R, C, "x"), w, b, _rows(out, N, R, C, "out"), mean.data_ptr(), rstd.data_ptr(), N, R, C, eps, code, pcode)
+    return out, mean, rstd
 
 
 def liec_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, weight: Optional[torch.Tensor] = None,
@@ -210,30 +237,32 @@ def liec_layer_norm_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tens
     """Gradients of liec_layer_norm: returns dx (a new tensor unless one is given, which may be dy or x; None with
     need_dx=False) and writes the gradients of weight and bias into dweight and dbias where they are given: [N, C] takes
     each worker's own sum (columns of the gradient rows of a step, say), [C] the sum over everything."""
-    code = _activations_type(x)
+    code, device = _dtype_code(x.dtype), x.get_device()
+    if code is None or device < 0:
+        raise TypeError("activations must be float32, bfloat16 or float16 on the GPU")
     N, R, C = _workers_of(x, (weight, dweight, dbias))
-    like = weight if weight is not None else dweight if dweight is not None else dbias
-    if N == 1 and not dy.is_contiguous() and dy.dim() == 3 and dy.shape == x.shape and x.shape[0]:
+    _like(dy, x, "dy")
+    if N == 1 and dy.dim() == 3 and x.shape[0] and not dy.is_contiguous():
         N, R = x.shape[0], x.shape[1]                          # one weight for all: any split of the rows will do
-    w, dw, db = _param(weight, like, x), _param(dweight, like, x), _param(dbias, like, x)
+    ptype, pcode = _param_type(weight, dweight, dbias)
+    w, dw, db = _param(weight, ptype, device), _param(dweight, ptype, device), _param(dbias, ptype, device)
+    lead = x.shape[:-1]
     for s in (mean, rstd):
-        if s.dtype != torch.float32 or s.get_device() != x.get_device() or s.shape != x.shape[:-1] or not s.is_contiguous():
+        if s.dtype != torch.float32 or s.get_device() != device or s.shape != lead or not s.is_contiguous():
             raise TypeError("mean and rstd must be what liec_layer_norm returned")
     if not need_dx:
         dx = None
     elif dx is None:
         dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    gr, xr = _rows(dy, N, R, C, x, "dy"), _rows(x, N, R, C, x, "x")
-    dr = None if dx is None else _rows(dx, N, R, C, x, "dx")
-    device = x.get_device()
+    else:
+        _like(dx, x, "dx")
     ws, need = None, 0
     if dw is not None or db is not None:
-        need = int(lib().liec_layer_norm_workspace(N, R, C))
+        need = lib().liec_layer_norm_workspace(N, R, C)
         if need < 0:
             raise ValueError(f"{N} workers of {R} rows of {C} columns are more than the library takes")
-        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
-    with _on(device):
-        _check(lib().liec_layer_norm_backward(ctypes.byref(gr), ctypes.byref(xr), mean.data_ptr(), rstd.data_ptr(), _ref(w), _ref(dr), _ref(dw),
-                                              _ref(db), N, R, C, code, 0 if like is None else _DTYPES[like.dtype], _optional(ws), need,
-                                              _stream(device)), "liec_layer_norm_backward")
+        if need:
+            ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _call("liec_layer_norm_backward", device, _rows(dy, N, R, C, "dy"), _rows(x, N, R, C, "x"), mean.data_ptr(), rstd.data_ptr(), w,
+          None if dx is None else _rows(dx, N, R, C, "dx"), dw, db, N, R, C, code, pcode, _optional(ws), need)
     return dx
