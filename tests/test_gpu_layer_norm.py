@@ -115,7 +115,8 @@ def test_every_row_length(C, dtype):
 
 
 @pytest.mark.parametrize("N,R,C", [(1, 5000, 64), (1, 3000, 24), (7, 1030, 40), (2, 4097, 257), (1, 9001, 1001), (5, 300, 4096), (70, 33, 130),
-                                   (1, 2000, 8200), (3, 513, 16_384), (2, 700, 20_000), (3, 700, 5)])
+                                   (1, 2000, 8200), (3, 513, 16_384), (1, 3001, 4100), (1, 2500, 4096), (1, 6001, 2048), (1, 1501, 8192),
+                                   (1, 5003, 1024), (2, 20_001, 16), (1, 12_007, 512), (2, 700, 20_000), (3, 700, 5)])
 @pytest.mark.parametrize("dtype", list(DTYPES))
 def test_many_rows(N, R, C, dtype):
     say(f"case layer norm N={N} R={R} C={C} {dtype}")
