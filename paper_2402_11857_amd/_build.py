@@ -46,5 +46,33 @@ def build_library(verbose: bool = False, defines=(), out: str = LIB_PATH) -> str
     return out
 
 
+BINDING_PATH = os.path.join(_HERE, "_train.so")
+
+
+def build_binding(verbose: bool = False) -> str:
+    """Always recompiles the Python side of include/liec_train.h (host code only, against torch's headers)."""
+    import sysconfig
+
+    from torch.utils import cpp_extension
+
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if not cxx:
+        raise RuntimeError("g++ not found: the binding cannot be built")
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-I", os.path.join(_ROOT, "include")]
+    for path in cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]:
+        cmd += ["-isystem", path]
+    cmd += [os.path.join(_HERE, "csrc", "train_binding.cpp"), "-o", BINDING_PATH]
+    for path in cpp_extension.library_paths():
+        cmd += ["-L", path]
+    cmd += ["-lc10", "-ltorch_cpu", "-ltorch_python"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("the binding did not compile:\n" + res.stdout + res.stderr)
+    return BINDING_PATH
+
+
 if __name__ == "__main__":
     print(build_library(verbose=True))
+    print(build_binding(verbose=True))
