@@ -4,8 +4,7 @@
  * global norm of a worker's gradient tensors, and clipping by it, in place or on the way into the fp32 rows of
  * liec_step.
  *
- * Tensors are DEVICE pointers of one of the types of liec_dtype, at any multiple of the element's size (16-byte
- * multiples are a little faster).  The entry points need no context and allocate nothing: they enqueue kernels on
+ * Tensors are DEVICE pointers of one of the types of liec_dtype, at any multiple of the element's size.  The entry points need no context and allocate nothing: they enqueue kernels on
  * `hip_stream` (a hipStream_t passed as void*, NULL = null stream) of the current device and return.  Where scratch
  * is needed the caller passes it (`workspace`, 16-byte aligned DEVICE memory of at least the bytes that the matching
  * *_workspace call names; its contents need no preparation, and calls that may overlap need one each).  They may be
@@ -97,8 +96,9 @@ typedef struct {
  * y = (x - mu) * rstd * weight + bias.
  *   mean, rstd   DEVICE fp32 [N, R] contiguous, for the backward pass; either may be NULL
  *   dtype        type of x and y;  param_dtype  type of weight and bias
- *   1 <= N <= 65535, 0 <= R < 2^31 (no rows: nothing to do), 1 <= C < 2^31, eps >= 0 and finite
- * y may be x itself (same pointer and strides); otherwise they must not overlap.  Rows of 8 to 16384 columns are read
+ *   1 <= N <= 65535, 0 <= R < 2^31 (no rows: nothing to do), 1 <= C <= 2^28, at most 2^40 values, eps >= 0 and
+ *                finite; no value lies further than 2^40 values from the first
+ * y may be x itself (same pointer and strides); otherwise they must not overlap, and neither may y's rows one another.  Rows of 8 to 16384 columns are read
  * once.
  */
 liec_status liec_layer_norm(const liec_rows *x, const liec_param *weight, const liec_param *bias, const liec_rows *y,
@@ -114,7 +114,8 @@ int64_t liec_layer_norm_workspace(int32_t N, int64_t R, int64_t C);
  *   dx = rstd * (a - mean(a) - h * mean(a h)),  dweight_i = sum over worker i's rows of dy * h,  dbias_i of dy.
  * dweight and dbias with stride 0 take the sum over all workers' rows.  They are written, not added to, also where
  * there are no rows (zeros).
- *   dx           NULL, or data = NULL, where it is not asked for; dx may be dy or x itself (same pointer and strides)
+ *   dx           NULL, or data = NULL, where it is not asked for; dx may be dy or x itself (same pointer and strides);
+ *                its rows must not overlap
  *   mean, rstd   as liec_layer_norm left them
  *   param_dtype  type of weight, dweight and dbias
  */

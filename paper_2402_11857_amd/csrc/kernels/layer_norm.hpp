@@ -199,39 +199,41 @@ __global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock)) void k_ln_forward(uint
     }
 }
 
-// Rows of any length: one block per row, which it reads three times (from the caches after the first).
+// Rows of any length: a block to a row, which it reads three times (from the caches after the first).
 template <typename T>
 __global__ __launch_bounds__(kLnWide) void k_ln_forward_wide(int64_t C, float eps, int64_t R, float* __restrict__ mean, float* __restrict__ rstd,
                                                              LnRows x, LnRows y, LnParam w, LnParam b) {
     __shared__ double lds_w[kLnWide / 64];
     const uint32_t worker = blockIdx.y;
-    const int64_t r = blockIdx.x;
-    const T* const xr = static_cast<const T*>(x.data) + (int64_t)worker * x.worker + r * x.row;
-    T* const yr = static_cast<T*>(y.data) + (int64_t)worker * y.worker + r * y.row;
-    double acc = 0.0;
-    for (int64_t j = threadIdx.x; j < C; j += blockDim.x) acc += (double)widen(xr[j]);
-    acc = block_sum_f64(acc, lds_w);
-    if (threadIdx.x == 0) lds_w[0] = acc / (double)C;
-    __syncthreads();
-    const double mu = lds_w[0];
-    __syncthreads();
-    acc = 0.0;
-    for (int64_t j = threadIdx.x; j < C; j += blockDim.x) {
-        const double d = (double)widen(xr[j]) - mu;
-        acc = __fma_rn(d, d, acc);
-    }
-    acc = block_sum_f64(acc, lds_w);
-    if (threadIdx.x == 0) lds_w[0] = acc / (double)C;
-    __syncthreads();
-    const float rs = (float)(1.0 / __dsqrt_rn(lds_w[0] + (double)eps)), m = (float)mu;
-    for (int64_t j = threadIdx.x; j < C; j += blockDim.x) {
-        const float wj = w.data ? load_any(w.data, (int64_t)worker * w.stride + j, w.type) : 1.f;
-        const float bj = b.data ? load_any(b.data, (int64_t)worker * b.stride + j, b.type) : 0.f;
-        yr[j] = narrow<T>(__fmaf_rn((widen(xr[j]) - m) * rs, wj, bj));
-    }
-    if (threadIdx.x == 0) {
-        if (mean) mean[(int64_t)worker * R + r] = m;
-        if (rstd) rstd[(int64_t)worker * R + r] = rs;
+    for (int64_t r = blockIdx.x; r < R; r += gridDim.x) {
+        const T* const xr = static_cast<const T*>(x.data) + (int64_t)worker * x.worker + r * x.row;
+        T* const yr = static_cast<T*>(y.data) + (int64_t)worker * y.worker + r * y.row;
+        double acc = 0.0;
+        for (int64_t j = threadIdx.x; j < C; j += blockDim.x) acc += (double)widen(xr[j]);
+        acc = block_sum_f64(acc, lds_w);
+        if (threadIdx.x == 0) lds_w[0] = acc / (double)C;
+        __syncthreads();
+        const double mu = lds_w[0];
+        __syncthreads();
+        acc = 0.0;
+        for (int64_t j = threadIdx.x; j < C; j += blockDim.x) {
+            const double d = (double)widen(xr[j]) - mu;
+            acc = __fma_rn(d, d, acc);
+        }
+        acc = block_sum_f64(acc, lds_w);
+        if (threadIdx.x == 0) lds_w[0] = acc / (double)C;
+        __syncthreads();
+        const float rs = (float)(1.0 / __dsqrt_rn(lds_w[0] + (double)eps)), m = (float)mu;
+        for (int64_t j = threadIdx.x; j < C; j += blockDim.x) {
+            const float wj = w.data ? load_any(w.data, (int64_t)worker * w.stride + j, w.type) : 1.f;
+            const float bj = b.data ? load_any(b.data, (int64_t)worker * b.stride + j, b.type) : 0.f;
+            yr[j] = narrow<T>(__fmaf_rn((widen(xr[j]) - m) * rs, wj, bj));
+        }
+        if (threadIdx.x == 0) {
+            if (mean) mean[(int64_t)worker * R + r] = m;
+            if (rstd) rstd[(int64_t)worker * R + r] = rs;
+        }
+        __syncthreads();                                    // lds_w is the next row's
     }
 }
 
@@ -419,35 +421,37 @@ __global__ __launch_bounds__(kBlock) void k_ln_param_grads(const float* __restri
     }
 }
 
-// Rows of any length: dx, one block per row.
+// Rows of any length: dx, a block to a row.
 template <typename T>
 __global__ __launch_bounds__(kLnWide) void k_ln_backward_wide(int64_t C, int64_t R, const float* __restrict__ mean, const float* __restrict__ rstd,
                                                               LnRows dy, LnRows x, LnRows dx, LnParam w) {
     __shared__ double lds_w[2][kLnWide / 64];
     const uint32_t worker = blockIdx.y;
-    const int64_t r = blockIdx.x;
-    const T* const xr = static_cast<const T*>(x.data) + (int64_t)worker * x.worker + r * x.row;
-    const T* const gr = static_cast<const T*>(dy.data) + (int64_t)worker * dy.worker + r * dy.row;
-    T* const out = static_cast<T*>(dx.data) + (int64_t)worker * dx.worker + r * dx.row;
-    const float mu = mean[(int64_t)worker * R + r], rs = rstd[(int64_t)worker * R + r];
     auto weight = [&](int64_t j) { return w.data ? load_any(w.data, (int64_t)worker * w.stride + j, w.type) : 1.f; };
-    double s1 = 0.0, s2 = 0.0;
-    for (int64_t j = threadIdx.x; j < C; j += blockDim.x) {
-        const float a = widen(gr[j]) * weight(j);
-        s1 += (double)a;
-        s2 += (double)a * (double)((widen(xr[j]) - mu) * rs);
-    }
-    s1 = block_sum_f64(s1, lds_w[0]);
-    s2 = block_sum_f64(s2, lds_w[1]);
-    if (threadIdx.x == 0) {
-        lds_w[0][0] = s1 / (double)C;
-        lds_w[1][0] = s2 / (double)C;
-    }
-    __syncthreads();
-    const float c1 = (float)lds_w[0][0], c2 = (float)lds_w[1][0];
-    for (int64_t j = threadIdx.x; j < C; j += blockDim.x) {
-        const float h = (widen(xr[j]) - mu) * rs;
-        out[j] = narrow<T>(rs * __fmaf_rn(-h, c2, widen(gr[j]) * weight(j) - c1));
+    for (int64_t r = blockIdx.x; r < R; r += gridDim.x) {
+        const T* const xr = static_cast<const T*>(x.data) + (int64_t)worker * x.worker + r * x.row;
+        const T* const gr = static_cast<const T*>(dy.data) + (int64_t)worker * dy.worker + r * dy.row;
+        T* const out = static_cast<T*>(dx.data) + (int64_t)worker * dx.worker + r * dx.row;
+        const float mu = mean[(int64_t)worker * R + r], rs = rstd[(int64_t)worker * R + r];
+        double s1 = 0.0, s2 = 0.0;
+        for (int64_t j = threadIdx.x; j < C; j += blockDim.x) {
+            const float a = widen(gr[j]) * weight(j);
+            s1 += (double)a;
+            s2 += (double)a * (double)((widen(xr[j]) - mu) * rs);
+        }
+        s1 = block_sum_f64(s1, lds_w[0]);
+        s2 = block_sum_f64(s2, lds_w[1]);
+        if (threadIdx.x == 0) {
+            lds_w[0][0] = s1 / (double)C;
+            lds_w[1][0] = s2 / (double)C;
+        }
+        __syncthreads();
+        const float c1 = (float)lds_w[0][0], c2 = (float)lds_w[1][0];
+        for (int64_t j = threadIdx.x; j < C; j += blockDim.x) {
+            const float h = (widen(xr[j]) - mu) * rs;
+            out[j] = narrow<T>(rs * __fmaf_rn(-h, c2, widen(gr[j]) * weight(j) - c1));
+        }
+        __syncthreads();                                    // lds_w is the next row's
     }
 }
 

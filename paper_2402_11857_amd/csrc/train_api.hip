@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "kernels/grads.hpp"
@@ -185,6 +186,8 @@ liec_status run_grads(const GradCall& c) {
 // ---- layer normalisation ---------------------------------------------------------------------------------------------
 constexpr int64_t kLnMost = 16384;                                   // columns that a team holds
 
+constexpr int64_t kLnWideBlocks = 65536;                             // that walk rows no team holds
+
 struct Team {
     int lanes, eights;                 // lanes to a row, columns of a lane in eights
 };
@@ -235,12 +238,21 @@ Strips backward_strips(int32_t N, int64_t R, int64_t C) {
     return strips_of(N, R, C, backward_waves(C));
 }
 
-bool valid_rows(const liec_rows* r, int64_t size) {
-    const int64_t most = (int64_t)1 << 44;
-    return r && r->data && aligned_to(r->data, size) && llabs(r->worker_stride) <= most && llabs(r->row_stride) <= most;
+constexpr int64_t kMostValues = (int64_t)1 << 40;
+bool in_range(int64_t stride) { return stride >= -kMostValues && stride <= kMostValues; }
+bool valid_rows(const liec_rows* r, int32_t N, int64_t R, int64_t size) {
+    if (!r || !r->data || !aligned_to(r->data, size) || !in_range(r->worker_stride) || !in_range(r->row_stride)) return false;
+    return (double)(R - 1) * (double)llabs(r->row_stride) + (double)(N - 1) * (double)llabs(r->worker_stride) <= (double)kMostValues;
 }
-bool valid_param(const liec_param* p, int64_t size) {
-    return !p || !p->data || (aligned_to(p->data, size) && llabs(p->stride) <= (int64_t)1 << 44);
+bool valid_param(const liec_param* p, int64_t size) { return !p || !p->data || (aligned_to(p->data, size) && in_range(p->stride)); }
+// Rows that are written must not share memory: the wider of the two strides spans what the narrower one covers.
+bool apart(const liec_rows* r, int32_t N, int64_t R, int64_t C) {
+    int64_t s = llabs(r->row_stride), n = R, wide = llabs(r->worker_stride), many = N;
+    if (many == 1 || (n > 1 && wide < s)) {
+        std::swap(s, wide);
+        std::swap(n, many);
+    }
+    return (n == 1 || s >= C) && (many == 1 || wide >= (n - 1) * s + C);
 }
 bool same(const liec_rows* a, const liec_rows* b) {
     return a->data == b->data && a->worker_stride == b->worker_stride && a->row_stride == b->row_stride;
@@ -260,7 +272,8 @@ LnRows rows_of(const liec_rows* r) { return r ? LnRows{r->data, r->worker_stride
 LnParam param_of(const liec_param* p, int type) { return p && p->data ? LnParam{p->data, p->stride, (uint32_t)type} : LnParam{nullptr, 0, (uint32_t)type}; }
 
 bool valid_sizes(int32_t N, int64_t R, int64_t C) {
-    return N >= 1 && N <= kMaxWorkers && R >= 0 && R < ((int64_t)1 << 31) && C >= 1 && C < ((int64_t)1 << 31);
+    if ((double)N * (double)R * (double)C > (double)kMostValues) return false;
+    return N >= 1 && N <= kMaxWorkers && R >= 0 && R < ((int64_t)1 << 31) && C >= 1 && C <= ((int64_t)1 << 28);
 }
 
 struct LnForward {
@@ -295,7 +308,7 @@ void run_forward(const LnForward& a) {
 template <typename T>
 void forward_of(const LnForward& a) {
     if (!holds(a.C)) {
-        k_ln_forward_wide<T><<<dim3((uint32_t)a.R, (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.eps, a.R, a.mean, a.rstd, a.x, a.y, a.w, a.b);
+        k_ln_forward_wide<T><<<dim3((uint32_t)std::min(a.R, kLnWideBlocks), (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.eps, a.R, a.mean, a.rstd, a.x, a.y, a.w, a.b);
         return;
     }
     const Team t = team_of(a.C);
@@ -347,7 +360,7 @@ void backward_of(const LnBackward& a) {
             k_ln_columns_wide<T><<<dim3((uint32_t)ceil_div(a.C, kBlock), (uint32_t)a.N, (uint32_t)a.strips.count), kBlock, 0, a.st>>>(
                 a.C, a.strips.per, a.R, a.partial, a.mean, a.rstd, a.dy, a.x);
         if (a.dx.data)
-            k_ln_backward_wide<T><<<dim3((uint32_t)a.R, (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.R, a.mean, a.rstd, a.dy, a.x, a.dx, a.w);
+            k_ln_backward_wide<T><<<dim3((uint32_t)std::min(a.R, kLnWideBlocks), (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.R, a.mean, a.rstd, a.dy, a.x, a.dx, a.w);
         return;
     }
     const Team t = team_of(a.C);
@@ -424,8 +437,8 @@ liec_status liec_layer_norm(const liec_rows* x, const liec_param* weight, const 
     if (!valid_sizes(N, R, C) || !valid_type(dtype) || !valid_type(param_dtype) || !(eps >= 0.f) || !isfinite(eps)) return LIEC_EINVAL;
     if (R == 0) return LIEC_OK;
     const int64_t size = size_of(dtype), psize = size_of(param_dtype);
-    if (!valid_rows(x, size) || !valid_rows(y, size) || !valid_param(weight, psize) || !valid_param(bias, psize)) return LIEC_EINVAL;
-    if (!aligned_to(mean, 4) || !aligned_to(rstd, 4) || !may_write(y, x, N, R, C, size)) return LIEC_EINVAL;
+    if (!valid_rows(x, N, R, size) || !valid_rows(y, N, R, size) || !valid_param(weight, psize) || !valid_param(bias, psize)) return LIEC_EINVAL;
+    if (!aligned_to(mean, 4) || !aligned_to(rstd, 4) || (mean && mean == rstd) || !apart(y, N, R, C) || !may_write(y, x, N, R, C, size)) return LIEC_EINVAL;
     const LnForward a{rows_of(x), rows_of(y), param_of(weight, param_dtype), param_of(bias, param_dtype), mean, rstd, eps, N, R, C, (hipStream_t)hip_stream};
     if (dtype == LIEC_F32) forward_of<float>(a);
     else if (dtype == LIEC_BF16) forward_of<bf16>(a);
@@ -447,12 +460,13 @@ liec_status liec_layer_norm_backward(const liec_rows* dy, const liec_rows* x, co
     const bool params = (dweight && dweight->data) || (dbias && dbias->data);
     if (dx && !dx->data) dx = nullptr;
     if (R) {
-        if (!valid_rows(dy, size) || !valid_rows(x, size) || (dx && !valid_rows(dx, size))) return LIEC_EINVAL;
+        if (!valid_rows(dy, N, R, size) || !valid_rows(x, N, R, size) || (dx && !valid_rows(dx, N, R, size))) return LIEC_EINVAL;
         if (!mean || !rstd || !aligned_to(mean, 4) || !aligned_to(rstd, 4)) return LIEC_EINVAL;
-        if (dx && !(may_write(dx, dy, N, R, C, size) && may_write(dx, x, N, R, C, size))) return LIEC_EINVAL;
+        if (dx && !(apart(dx, N, R, C) && may_write(dx, dy, N, R, C, size) && may_write(dx, x, N, R, C, size))) return LIEC_EINVAL;
         if (params && !valid_workspace(workspace, workspace_bytes, liec_layer_norm_workspace(N, R, C))) return LIEC_EINVAL;
     }
     if (params) {
+        if (dweight && dbias && dweight->data && dweight->data == dbias->data) return LIEC_EINVAL;
         // one sum for all workers, or one for each: the same for both gradients
         if (dweight && dweight->data && dbias && dbias->data && N > 1 && (dweight->stride == 0) != (dbias->stride == 0)) return LIEC_EINVAL;
         if (N > 1)

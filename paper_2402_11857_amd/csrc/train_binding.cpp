@@ -106,6 +106,7 @@ struct Grads {
 };
 
 void read_grads(Grads& g, PyObject* list, const at::Tensor* norms, bool whole) {
+    if (THPVariable_Check(list)) type_error("gradients must be a sequence of tensors, not a tensor");
     g.sequence = PySequence_Fast(list, "gradients must be a sequence of tensors");
     if (!g.sequence) throw Raise{nullptr, ""};
     const Py_ssize_t T = PySequence_Fast_GET_SIZE(g.sequence);

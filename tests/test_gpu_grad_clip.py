@@ -287,7 +287,8 @@ def test_refusals():
                 lambda: pkg.liec_grad_norm([a.double()]),
                 lambda: pkg.liec_grad_norm([a], torch.empty(2, dtype=torch.float64, device=DEV)),
                 lambda: pkg.liec_gather_grads([a], rows.double()),
-                lambda: pkg.liec_grad_norm([a, a.cpu()])):
+                lambda: pkg.liec_grad_norm([a, a.cpu()]),
+                lambda: pkg.liec_grad_norm(a)):
         with pytest.raises(TypeError):
             bad()
     for bad in (lambda: pkg.liec_grad_norm([]),

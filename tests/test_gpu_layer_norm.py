@@ -116,7 +116,7 @@ def test_every_row_length(C, dtype):
 
 @pytest.mark.parametrize("N,R,C", [(1, 5000, 64), (1, 3000, 24), (7, 1030, 40), (2, 4097, 257), (1, 9001, 1001), (5, 300, 4096), (70, 33, 130),
                                    (1, 2000, 8200), (3, 513, 16_384), (1, 3001, 4100), (1, 2500, 4096), (1, 6001, 2048), (1, 1501, 8192),
-                                   (1, 5003, 1024), (2, 20_001, 16), (1, 12_007, 512), (2, 700, 20_000), (3, 700, 5)])
+                                   (1, 5003, 1024), (2, 20_001, 16), (1, 12_007, 512), (2, 700, 20_000), (3, 700, 5), (1, 70_001, 5)])
 @pytest.mark.parametrize("dtype", list(DTYPES))
 def test_many_rows(N, R, C, dtype):
     say(f"case layer norm N={N} R={R} C={C} {dtype}")
@@ -355,6 +355,9 @@ def test_refusals():
     for bad in (lambda: pkg.liec_layer_norm(x, w, b, eps=-1.0),
                 lambda: pkg.liec_layer_norm(x, w, b, eps=float("inf")),
                 lambda: pkg.liec_layer_norm(flat[:512].view(2, 4, 64), w, out=flat[8:].view(2, 4, 64)),          # they overlap
+                lambda: pkg.liec_layer_norm(x, w, out=torch.empty(2, 1, 64, device=DEV).expand(2, 4, 64)),
+                lambda: pkg.liec_layer_norm_backward(dy, x, mean, rstd, w, dx=torch.empty(1, 4, 64, device=DEV).expand(2, 4, 64)),
+                lambda: pkg.liec_layer_norm_backward(dy, x, mean, rstd, w, dweight=w, dbias=w),
                 lambda: pkg.liec_layer_norm_backward(dy, x, mean, rstd, w, dweight=torch.empty(2, 64, device=DEV), dbias=torch.empty(64, device=DEV))):
         with pytest.raises(pkg.LiecError):
             bad()

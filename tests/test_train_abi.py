@@ -33,6 +33,16 @@ def lib():
     return pkg.lib()
 
 
+@pytest.fixture(scope="module")
+def pkg(lib):
+    import paper_2402_11857_amd as package
+    from paper_2402_11857_amd import _build
+
+    if not os.path.exists(_build.BINDING_PATH):
+        _build.build_binding()
+    return package
+
+
 def test_every_declared_symbol_is_exported_and_bound(lib):
     import paper_2402_11857_amd as pkg
 
@@ -154,6 +164,13 @@ def test_layer_norm_refusals(lib):
     assert forward(mean=FAKE + 2) == 1
     assert forward(y=Rows(FAKE, 640, 65)) == 1               # the same start, other strides
     assert forward(y=Rows(FAKE + 64, 640, 64)) == 1          # dense, and they overlap
+    assert forward(y=Rows(1 << 30, 640, 63)) == 1            # rows of y overlap
+    assert forward(y=Rows(1 << 30, 0, 64)) == 1
+    assert forward(y=Rows(1 << 30, 64, 64)) == 1
+    assert forward(y=Rows(1 << 30, 32, 128)) == 1
+    assert forward(x=Rows(FAKE, -(1 << 63), 64)) == 1
+    assert forward(weight=Param(FAKE, -(1 << 63))) == 1
+    assert forward(C=(1 << 28) + 1) == 1
     assert forward(R=0) == 0                                 # no rows: nothing is looked at
 
     need = lib.liec_layer_norm_workspace(2, 10, 64)
@@ -166,8 +183,37 @@ def test_layer_norm_refusals(lib):
     assert backward(x=None) == 1
     assert backward(mean=None) == 1
     assert backward(dx=Rows(FAKE + 64, 640, 64)) == 1
+    assert backward(dx=Rows(1 << 30, 0, 64)) == 1
+    assert backward(db=w) == 1                               # one place for both gradients
     assert backward(ws=None) == 1
     assert backward(bytes=need - 1) == 1
     assert backward(dw=Param(FAKE, 63)) == 1                 # workers' gradients overlap
     assert backward(db=Param(FAKE, 0)) == 1                  # one shared, one not
     assert backward(N=0) == 1
+
+
+def test_binding_refuses_what_is_not_on_a_gpu_or_not_a_tensor(pkg):
+    import torch
+
+    x = torch.ones(2, 3, 8)
+    for bad in (lambda: pkg.liec_layer_norm(x),
+                lambda: pkg.liec_layer_norm(None),
+                lambda: pkg.liec_layer_norm([1.0]),
+                lambda: pkg.liec_layer_norm(x.double()),
+                lambda: pkg.liec_layer_norm(x, eps="small"),
+                lambda: pkg.liec_layer_norm_backward(x, x, x[..., 0], x[..., 0]),
+                lambda: pkg.liec_layer_norm_backward(x, x, None, x[..., 0]),
+                lambda: pkg.liec_grad_norm([x]),
+                lambda: pkg.liec_grad_norm([1.0]),
+                lambda: pkg.liec_grad_norm(3),
+                lambda: pkg.liec_grad_norm(x),                # one tensor where a list is expected
+                lambda: pkg.liec_clip_grads([x], "1"),
+                lambda: pkg.liec_gather_grads([x], None)):
+        with pytest.raises(TypeError):
+            bad()
+    with pytest.raises(ValueError):
+        pkg.liec_grad_norm([])
+    with pytest.raises(ValueError):
+        pkg.liec_grad_norm([x], workers=2)
+    with pytest.raises(TypeError):
+        pkg.train.native().grad_norm()
