@@ -79,7 +79,9 @@ __device__ __forceinline__ T* in_row(T* row, uint32_t at) {
 // The team that a thread belongs to, known to be the same for a whole wave where it is.
 template <int TEAM>
 __device__ __forceinline__ uint32_t team_index() {
-    return TEAM >= 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TEAM) : threadIdx.x / TEAM;
+    const uint32_t team = threadIdx.x / TEAM;
+    if (TEAM < 64) return team;
+    return __builtin_amdgcn_readfirstlane(team);
 }
 // Whether vector k may lie at or beyond the end of its row: rows that half as many vectors per lane hold take a smaller team,
 // except for the smallest one.
