@@ -191,20 +191,31 @@ constexpr int64_t kLnWideBlocks = 65536;                             // that wal
 struct Team {
     int lanes, eights;                 // lanes to a row, columns of a lane in eights
 };
-// The smallest team that holds a row.
-Team team_of(int64_t C) {
-    const int64_t v = ceil_div(C, 8);
-    if (v <= 8) return {8, 1};
-    if (v <= 16) return {16, 1};
-    if (v <= 32) return {32, 1};
-    if (v <= 64) return {64, 1};
-    if (v <= 128) return {64, 2};
-    if (v <= 256) return {128, 2};
-    if (v <= 512) return {256, 2};
-    if (v <= 1024) return {512, 2};
+// The smallest team that holds a row, for the forward pass, which has registers for four eights per lane (8 x 30000 rows of
+// 1024 bf16 columns 162 us, with 64 lanes of two 175; 200 MB in rows of 2000 64 against 73 with 128 lanes and a barrier), ...
+Team forward_team(int64_t C) {
+    if (C <= 64) return {8, 1};
+    if (C <= 128) return {16, 1};
+    if (C <= 256) return {16, 2};
+    if (C <= 512) return {32, 2};
+    if (C <= 1024) return {32, 4};
+    if (C <= 2048) return {64, 4};
+    if (C <= 4096) return {128, 4};
+    if (C <= 8192) return {256, 4};
+    return {512, 4};
+}
+// ... and for the backward pass, whose lanes also hold the weight gradients of their columns.
+Team backward_team(int64_t C) {
+    if (C <= 64) return {8, 1};
+    if (C <= 128) return {16, 1};
+    if (C <= 256) return {16, 2};
+    if (C <= 512) return {32, 2};
+    if (C <= 1024) return {64, 2};
+    if (C <= 2048) return {128, 2};
+    if (C <= 4096) return {256, 2};
+    if (C <= 8192) return {512, 2};
     return {1024, 2};
 }
-
 int64_t threads_of(const Team& t) { return t.lanes > 64 ? t.lanes : kBlock; }
 int64_t teams_of(const Team& t) { return threads_of(t) / t.lanes; }
 
@@ -213,29 +224,27 @@ bool holds(int64_t C) { return C >= kLnShortest && C <= kLnMost; }
 struct Strips {
     int64_t per, count;
 };
-// Rows of a block: as many blocks as are resident at a time, `waves` of them on each of the chip's 1024 SIMDs, and two rows
-// for each of a block's teams at least.
-Strips strips_of(int32_t N, int64_t R, int64_t C, int64_t waves) {
-    if (R == 0) return {1, 0};
-    if (!holds(C)) {                   // the columns' sums, a thread per column
-        const int64_t per = ceil_div(R, std::max<int64_t>(1, 1024 / N / ceil_div(C, kBlock)));
-        return {per, ceil_div(R, per)};
-    }
-    const Team t = team_of(C);
+// Rows of a block: `waves` on each of the chip's 1024 SIMDs, and two rows for each of a block's teams at least.
+Strips strips_of(int32_t N, int64_t R, const Team& t, int64_t waves) {
     const int64_t want = std::max<int64_t>(1, 1024 * 64 * waves / threads_of(t) / N);
     const int64_t per = std::max(ceil_div(R, want), 2 * teams_of(t));
     return {per, ceil_div(R, per)};
 }
 
-// Waves per SIMD of the backward kernel: its weight gradients stay in registers.  One vector per lane leaves room for four
-// waves (six: as fast or 2 to 30 % slower); of two per lane two waves that request two rows ahead beat four that request one
-// (2048 columns 156 against 166 us, 8192 286 against 299); 16 waves to a row are four by themselves.
-int64_t backward_waves(int64_t C) { return !holds(C) ? 1 : team_of(C).eights == 1 || team_of(C).lanes == 1024 ? 4 : 2; }
-
-// Strips of the backward kernel.  Up to 8 rows for each of a block's teams stay in one block, whose sums need no second kernel.
+// Strips of the backward pass, each with partial sums of its own: as many blocks as are resident at a time.  Weight gradients
+// stay in registers; one vector per lane leaves room for four waves (six: as fast or 2 to 30 % slower); of two per lane two
+// waves that request two rows ahead beat four that request one (2048 columns 156 against 166 us, 8192 286 against 299); 16
+// waves to a row are four by themselves.
 Strips backward_strips(int32_t N, int64_t R, int64_t C) {
-    if (holds(C) && R > 0 && R <= 8 * teams_of(team_of(C))) return {R, 1};
-    return strips_of(N, R, C, backward_waves(C));
+    if (R == 0) return {1, 0};
+    if (!holds(C)) {                   // the columns' sums, a thread per column
+        const int64_t per = ceil_div(R, std::max<int64_t>(1, 1024 / N / ceil_div(C, kBlock)));
+        return {per, ceil_div(R, per)};
+    }
+    const Team t = backward_team(C);
+    // few rows: one block, whose sums need no second kernel
+    if (R <= 8 * teams_of(t)) return {R, 1};
+    return strips_of(N, R, t, t.eights == 1 || t.lanes == 1024 ? 4 : 2);
 }
 
 constexpr int64_t kMostValues = (int64_t)1 << 40;
@@ -294,9 +303,9 @@ template <typename T, int TEAM, int EIGHTS>
 void run_forward(const LnForward& a) {
     constexpr int K = EIGHTS * 8 / Vec16<T>::n, threads = TEAM > 64 ? TEAM : kBlock;
     const bool full = a.C == TEAM * EIGHTS * 8;
-    // Many short-lived blocks: 8 x 8192 rows of 4096 bf16 columns 185 us, blocks that stay on the chip and request rows ahead
+    // Many short-lived blocks: 8 x 8192 rows of 4096 bf16 columns 181 us, blocks that stay on the chip and request rows ahead
     // 194 to 220, although every block reads the weights again.
-    const Strips s = strips_of(a.N, a.R, a.C, 64);
+    const Strips s = strips_of(a.N, a.R, Team{TEAM, EIGHTS}, 32);
     const bool keep = keeps(a.N, a.R, a.C, sizeof(T));
     const dim3 grid((uint32_t)s.count, (uint32_t)a.N);
     if (full)
@@ -311,17 +320,17 @@ void forward_of(const LnForward& a) {
         k_ln_forward_wide<T><<<dim3((uint32_t)std::min(a.R, kLnWideBlocks), (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.eps, a.R, a.mean, a.rstd, a.x, a.y, a.w, a.b);
         return;
     }
-    const Team t = team_of(a.C);
+    const Team t = forward_team(a.C);
     switch (t.lanes * t.eights) {
         case 8: return run_forward<T, 8, 1>(a);
         case 16: return run_forward<T, 16, 1>(a);
-        case 32: return run_forward<T, 32, 1>(a);
-        case 64: return run_forward<T, 64, 1>(a);
-        case 128: return run_forward<T, 64, 2>(a);
-        case 256: return run_forward<T, 128, 2>(a);
-        case 512: return run_forward<T, 256, 2>(a);
-        case 1024: return run_forward<T, 512, 2>(a);
-        default: return run_forward<T, 1024, 2>(a);
+        case 32: return run_forward<T, 16, 2>(a);
+        case 64: return run_forward<T, 32, 2>(a);
+        case 128: return run_forward<T, 32, 4>(a);
+        case 256: return run_forward<T, 64, 4>(a);
+        case 512: return run_forward<T, 128, 4>(a);
+        case 1024: return run_forward<T, 256, 4>(a);
+        default: return run_forward<T, 512, 4>(a);
     }
 }
 
@@ -363,12 +372,12 @@ void backward_of(const LnBackward& a) {
             k_ln_backward_wide<T><<<dim3((uint32_t)std::min(a.R, kLnWideBlocks), (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.R, a.mean, a.rstd, a.dy, a.x, a.dx, a.w);
         return;
     }
-    const Team t = team_of(a.C);
+    const Team t = backward_team(a.C);
     switch (t.lanes * t.eights) {
         case 8: return run_backward<T, 8, 1>(a);
         case 16: return run_backward<T, 16, 1>(a);
-        case 32: return run_backward<T, 32, 1>(a);
-        case 64: return run_backward<T, 64, 1>(a);
+        case 32: return run_backward<T, 16, 2>(a);
+        case 64: return run_backward<T, 32, 2>(a);
         case 128: return run_backward<T, 64, 2>(a);
         case 256: return run_backward<T, 128, 2>(a);
         case 512: return run_backward<T, 256, 2>(a);
