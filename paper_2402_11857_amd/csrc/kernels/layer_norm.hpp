@@ -5,9 +5,12 @@
 //              dw_j = sum over the worker's rows of dy_j h_j,  db_j = sum over them of dy_j
 //
 // A team of TEAM lanes holds one row in registers, K vectors of 16 bytes per lane, so that a row is read once; teams of up
-// to a wave add up inside the wave, larger ones through LDS.  All sums are fp32, of at most a few hundred terms in a chain.
+// to a wave add up inside the wave, larger ones through LDS.  All sums are fp32, of at most a few hundred terms in a chain; rows that no team holds take fp64.
 // The last vector of a row that is not a multiple of a vector long starts a vector's length before the row's end: what it
 // shares with the vector before it is left out of the sums and stored twice with the same value, and no access needs a branch.
+//
+// Both kernels are bound by memory.  Measured on 8 x 8192 rows of 4096 bf16 columns: forward 181 us (5.9 TB/s of x and y, a copy
+// of that size 6.6), backward 273 us (5.9 TB/s of dy, x and dx; 5 us of it add up 512 partial sums).
 #pragma once
 #include <type_traits>
 
