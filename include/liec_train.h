@@ -62,8 +62,8 @@ liec_status liec_grad_norm(const liec_grad_tensor *tensors, int32_t T, int32_t N
  * clips nothing.
  *   max_norm  >= 0, not NaN
  *   norms     NULL, or N fp32 values (DEVICE): the norms before clipping
- * For N > 1 a tensor's |stride| is at least its count, and no two tensors may share memory (LIEC_EINVAL where the
- * values of worker 0 overlap, for instance a tied tensor listed twice).
+ * No two tensors, nor two workers' values of one, may share memory (LIEC_EINVAL, for instance for a tied tensor that
+ * is listed twice).
  */
 liec_status liec_clip_grads(const liec_grad_tensor *tensors, int32_t T, int32_t N, float max_norm, float *norms,
                             void *workspace, int64_t workspace_bytes, void *hip_stream);

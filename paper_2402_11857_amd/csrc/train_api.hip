@@ -18,8 +18,8 @@ namespace {
 
 constexpr int32_t kMaxWorkers = 65535;
 constexpr int64_t kMaxGradValues = (int64_t)1 << 35;
-// Thread blocks of a launch that adds up squares, 16 per compute unit, twice what is resident at a time (16 x 11.7M fp32
-// values: 2048 blocks 136 us, 4096 114, 8192 125).
+// Thread blocks of a launch that adds up squares, 16 per compute unit, twice what is resident at a time (norm of 16 x 11.7M
+// fp32 values: 2048 blocks 123 us, 4096 114).
 constexpr int64_t kGradBlocks = 4096;
 // Partial sums of a worker that the blocks of the scaling kernel add up again, each of them (138M values of one worker
 // clipped: 512 blocks 283 us, 1024 263, 2048 273, 4096 295).
@@ -74,6 +74,40 @@ bool ranges_meet(uintptr_t a, int64_t an, int64_t as, uintptr_t b, int64_t bn, i
     return (off < an && row <= last && row >= -last) || (off + bn > as && row + 1 <= last && row + 1 >= -last);
 }
 
+// Do any two tensors, or two workers' values of one, share memory?  May throw std::bad_alloc.
+bool grads_meet(const liec_grad_tensor* t, int32_t T, int32_t N) {
+    struct Range {
+        uintptr_t first, lo, hi;              // worker 0's start; where the values of all workers lie
+        int64_t bytes, stride;
+    };
+    std::vector<Range> all;
+    all.reserve((size_t)T);
+    bool matrix = N > 1;                      // columns of one matrix of N rows
+    for (int32_t i = 0; i < T; ++i) {
+        if (!t[i].count) continue;
+        if (N > 1 && llabs(t[i].stride) < t[i].count) return true;
+        const int64_t size = size_of(t[i].dtype), stride = N > 1 ? t[i].stride * size : 0, reach = stride * (N - 1);
+        const uintptr_t p = (uintptr_t)t[i].data;
+        all.push_back({p, p + (uintptr_t)std::min<int64_t>(0, reach), p + (uintptr_t)(std::max<int64_t>(0, reach) + t[i].count * size), t[i].count * size, stride});
+        matrix = matrix && stride > 0 && stride == all[0].stride;
+    }
+    std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
+    // starts and ends within one row of the matrix: neighbours are all there is to compare
+    matrix = matrix && !all.empty() && all.back().first - all[0].first < (uintptr_t)all[0].stride;
+    for (const Range& r : all) matrix = matrix && r.first + (uintptr_t)r.bytes <= all[0].first + (uintptr_t)all[0].stride;
+    uintptr_t reached = 0;                    // by the tensors before
+    for (size_t i = 0; i < all.size(); ++i) {
+        if (matrix) {
+            if (i && all[i].first < all[i - 1].first + (uintptr_t)all[i - 1].bytes) return true;
+            continue;
+        }
+        for (size_t j = 0; j < i && all[i].lo < reached; ++j)
+            if (all[j].hi > all[i].lo && ranges_meet(all[j].first, all[j].bytes, all[j].stride, all[i].first, all[i].bytes, all[i].stride, N)) return true;
+        reached = std::max(reached, all[i].hi);
+    }
+    return false;
+}
+
 struct GradBatch {
     int32_t first, count;
     int64_t tiles, blocks, col;               // col: column of its first tensor
@@ -87,7 +121,8 @@ struct GradPlan {
 // `rows`: workers that a launch works on.
 bool plan_grads(const liec_grad_tensor* t, int32_t T, int32_t N, int64_t rows, bool scales, GradPlan* out) {
     try {
-        const int64_t most = std::min(grad_parts_per_batch(N, T), std::max<int64_t>(1, std::min<int64_t>(kGradBlocks / rows, scales ? kGradParts : kGradBlocks))), share = ceil_div(T, grad_batches(T));
+        const int64_t wanted = std::max<int64_t>(1, std::min(kGradBlocks / rows, scales ? kGradParts : kGradBlocks));
+        const int64_t most = std::min(grad_parts_per_batch(N, T), wanted), share = ceil_div(T, grad_batches(T));
         int64_t col = 0;
         out->parts = out->bytes = 0;
         out->batches.clear();
@@ -409,17 +444,7 @@ liec_status liec_clip_grads(const liec_grad_tensor* tensors, int32_t T, int32_t 
     if (!valid_grads(tensors, T, N, &total) || !aligned_to(norms, 4) || !(max_norm >= 0.f)) return LIEC_EINVAL;
     if (!valid_workspace(workspace, workspace_bytes, liec_grads_workspace(N, T))) return LIEC_EINVAL;
     try {
-        std::vector<std::pair<uintptr_t, uintptr_t>> at;       // where worker 0's values start and end
-        at.reserve((size_t)T);
-        for (int32_t i = 0; i < T; ++i) {
-            if (!tensors[i].count) continue;
-            if (N > 1 && llabs(tensors[i].stride) < tensors[i].count) return LIEC_EINVAL;
-            const uintptr_t p = (uintptr_t)tensors[i].data;
-            at.emplace_back(p, p + (uintptr_t)(tensors[i].count * size_of(tensors[i].dtype)));
-        }
-        std::sort(at.begin(), at.end());
-        for (size_t i = 1; i < at.size(); ++i)
-            if (at[i].first < at[i - 1].second) return LIEC_EINVAL;
+        if (grads_meet(tensors, T, N)) return LIEC_EINVAL;
     } catch (const std::bad_alloc&) {
         return LIEC_ENOMEM;
     }

@@ -129,6 +129,11 @@ def test_clip_and_gather_refusals(lib):
     assert clip([t], float("nan")) == 1
     assert clip([Tensor(FAKE, 10, 9, 0, 0)]) == 1            # workers overlap
     assert clip([t, Tensor(FAKE + 36, 10, 10, 0, 0)]) == 1   # tensors overlap
+    assert clip([t, Tensor(FAKE + 40, 10, 10, 0, 0)]) == 1   # the second worker of one is the first of the other
+    assert clip([Tensor(FAKE, 10, 40, 0, 0), Tensor(FAKE + 40, 10, 40, 0, 0), Tensor(FAKE + 76, 10, 40, 0, 0)]) == 1     # columns of a matrix
+    assert clip([Tensor(FAKE, 10, 40, 0, 0), Tensor(FAKE + 128, 10, 40, 0, 0)]) == 1     # one reaches into the next row
+    assert clip([Tensor(FAKE, 10, 40, 0, 0), Tensor(FAKE + 40, 10, 41, 0, 0)]) == 1      # other distances: taken to meet
+    assert clip([Tensor(FAKE, 3, 0, 0, 0)]) == 1
     far = 1 << 30
     assert gather([t], None, 10) == 1
     assert gather([t], far + 2, 10) == 1
