@@ -50,7 +50,8 @@ int64_t liec_grads_workspace(int32_t N, int32_t T);
  * liec_grad_norm: norms[i] = sqrt(sum over the T tensors of the squares of worker i's values), i < N (DEVICE, fp32,
  * N values).  Infinities and NaN show in the norm of their worker, and only there.  T = 0 or no values: zero.
  *   1 <= N <= 65535, 0 <= T <= LIEC_GRAD_MAX_TENSORS, at most 2^35 values per worker.  stride may be anything, 0
- *   included (workers that share a tensor).  Two kernels (one more for each further 128 tensors).
+ *   included (workers that share a tensor).  Two kernels; one more for every 184 further
+ *   tensors (128 where a tensor's stride is not its count).
  */
 liec_status liec_grad_norm(const liec_grad_tensor *tensors, int32_t T, int32_t N, float *norms, void *workspace,
                            int64_t workspace_bytes, void *hip_stream);
@@ -73,7 +74,7 @@ liec_status liec_clip_grads(const liec_grad_tensor *tensors, int32_t T, int32_t 
  * liec_step reads: worker i's values of tensor t go to rows + i * row_stride + (counts of the tensors before t).
  * The tensors are read only (any stride); a tensor that shares memory with the rows is LIEC_EINVAL.
  *   row_stride  >= the sum of the counts
- *   max_norm = +Inf with norms = NULL only gathers: one kernel per 128 tensors, each value read once.
+ *   max_norm = +Inf with norms = NULL only gathers: one kernel for up to 128 tensors, each value read once.
  */
 liec_status liec_gather_grads(const liec_grad_tensor *tensors, int32_t T, int32_t N, float *rows, int64_t row_stride,
                               float max_norm, float *norms, void *workspace, int64_t workspace_bytes, void *hip_stream);

@@ -14,16 +14,30 @@ namespace liec {
 
 constexpr int kGradTile = 16384;
 constexpr int kGradVecs = kGradTile / (kBlock * 16);    // 16-byte vectors of a thread
-constexpr int kGradTensors = 128;      // tensors of one launch: what 4 KiB of kernel arguments hold
 
-// Tensors of one launch.  Tensor t has tiles first[t] .. first[t + 1] - 1 of every worker and columns col[t] .. col[t + 1] - 1
-// of a worker's row; worker i's elements start at data[t] + i * stride[t] (in elements).
+// Tensors of one launch: as many as 4 KiB of kernel arguments hold, more where every tensor's workers follow one another and no
+// distances are needed (161 tensors in one launch instead of two).  Tensor t has tiles first[t] .. first[t + 1] - 1 of every
+// worker and columns col[t] .. col[t + 1] - 1 of a worker's row; worker i's elements start at data[t] + i * stride(t) elements.
+template <bool STRIDED>
 struct GradTable {
-    const void* data[kGradTensors];
-    int64_t stride[kGradTensors];
-    int64_t col[kGradTensors + 1];
-    uint32_t first[kGradTensors + 1];
-    uint8_t type[kGradTensors];
+    static constexpr int most = 128;
+    const void* data[most];
+    int64_t strides[most];
+    int64_t col[most + 1];
+    uint32_t first[most + 1];
+    uint8_t type[most];
+    __device__ __forceinline__ int64_t stride(uint32_t t) const { return strides[t]; }
+    void set_stride(int i, int64_t s) { strides[i] = s; }
+};
+template <>
+struct GradTable<false> {
+    static constexpr int most = 184;
+    const void* data[most];
+    int64_t col[most + 1];
+    uint32_t first[most + 1];
+    uint8_t type[most];
+    __device__ __forceinline__ int64_t stride(uint32_t t) const { return col[t + 1] - col[t]; }
+    void set_stride(int, int64_t) {}
 };
 
 struct GradPass {
@@ -43,21 +57,27 @@ struct Tile {
     int64_t col;                       // column of its first element
 };
 
-// The tensor that holds tile `tile`: the last one that starts at or before it.  Every lane looks at two starts.
-__device__ __forceinline__ uint32_t tensor_of(const GradTable& tab, uint32_t count, uint32_t tile) {
+// The tensor that holds tile `tile`: the last one that starts at or before it.  Every lane looks at three starts.
+template <bool STRIDED>
+__device__ __forceinline__ uint32_t tensor_of(const GradTable<STRIDED>& tab, uint32_t count, uint32_t tile) {
     const uint32_t lane = threadIdx.x & 63;
-    const uint64_t a = __ballot(lane < count && tab.first[min(lane, count)] <= tile);
-    const uint64_t b = __ballot(lane + 64 < count && tab.first[min(lane + 64, count)] <= tile);
-    return __builtin_amdgcn_readfirstlane((uint32_t)(__popcll(a) + __popcll(b)) - 1u);
+    uint32_t before = 0;
+#pragma unroll
+    for (uint32_t q = 0; q < GradTable<STRIDED>::most; q += 64) {
+        const uint64_t in = __ballot(lane + q < count && tab.first[min(lane + q, count)] <= tile);
+        before += (uint32_t)__popcll(in);
+    }
+    return __builtin_amdgcn_readfirstlane(before - 1u);
 }
 
 // Tile `tile` of worker `row`; t: the tensor of an earlier tile, moved to this one's.
-__device__ __forceinline__ Tile tile_at(const GradTable& tab, uint32_t tile, uint32_t row, uint32_t& t) {
+template <bool STRIDED>
+__device__ __forceinline__ Tile tile_at(const GradTable<STRIDED>& tab, uint32_t tile, uint32_t row, uint32_t& t) {
     while (tile >= tab.first[t + 1]) ++t;
     const uint32_t type = tab.type[t], shift = type == kF32 ? 2 : 1;
     const int64_t off = (int64_t)(tile - tab.first[t]) * kGradTile, len = (tab.col[t + 1] - tab.col[t]) << shift;
     Tile r;
-    r.p = static_cast<char*>(const_cast<void*>(tab.data[t])) + (((int64_t)row * tab.stride[t]) << shift) + off;
+    r.p = static_cast<char*>(const_cast<void*>(tab.data[t])) + (((int64_t)row * tab.stride(t)) << shift) + off;
     r.bytes = (uint32_t)min((int64_t)kGradTile, len - off);
     r.type = type;
     r.col = tab.col[t] + (off >> shift);
@@ -111,8 +131,8 @@ __device__ __forceinline__ void square_tile(const Tile& c, const v4u (&r)[kGradV
 
 // Block b of a worker: every gridDim.x-th tile from b on, their sum of squares into partial[row][slot + b].  NT: past the caches,
 // where nothing reads the gradients again (32 x 25.6M bf16 values 252 us, through them 282).
-template <bool NT>
-__global__ __launch_bounds__(kBlock) void k_grad_squares(GradPass a, GradTable tab) {
+template <bool NT, bool STRIDED>
+__global__ __launch_bounds__(kBlock) void k_grad_squares(GradPass a, GradTable<STRIDED> tab) {
     __shared__ double lds_w[4];
     const uint32_t row = a.row + blockIdx.y;
     const uint32_t begin = blockIdx.x, end = a.tiles, B = gridDim.x;
@@ -214,8 +234,8 @@ __device__ __forceinline__ void scale_tile(const Tile& c, const v4u (&r)[kGradVe
 }
 
 // Tile b of a worker times its factor, which every block forms from the partial sums while its loads are under way.
-template <bool ROWS>
-__global__ __launch_bounds__(kBlock) void k_grad_scale(GradPass a, GradTable tab) {
+template <bool ROWS, bool STRIDED>
+__global__ __launch_bounds__(kBlock) void k_grad_scale(GradPass a, GradTable<STRIDED> tab) {
     __shared__ double lds_w[4];
     const uint32_t row = a.row + blockIdx.y;
     uint32_t t = tensor_of(tab, a.count, blockIdx.x);

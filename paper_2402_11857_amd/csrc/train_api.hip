@@ -36,7 +36,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 liec_status launched() { return hipGetLastError() == hipSuccess ? LIEC_OK : LIEC_EDEVICE; }
 
 // ---- gradients -------------------------------------------------------------------------------------------------------
-int64_t grad_batches(int32_t T) { return std::max<int64_t>(1, ceil_div(T, kGradTensors)); }
+// Launches that T tensors take, at most.
+int64_t grad_batches(int32_t T) { return std::max<int64_t>(1, ceil_div(T, GradTable<true>::most)); }
 
 // Partial sums of a worker that a launch may leave: what the workspace has room for.
 int64_t grad_parts_per_batch(int32_t N, int32_t T) {
@@ -115,6 +116,7 @@ struct GradBatch {
 
 struct GradPlan {
     int64_t parts = 0, bytes = 0;             // of a worker: partial sums, gradients
+    bool strided = false;                     // some tensor's workers do not follow one another
     std::vector<GradBatch> batches;           // those that have any values
 };
 
@@ -122,7 +124,10 @@ struct GradPlan {
 bool plan_grads(const liec_grad_tensor* t, int32_t T, int32_t N, int64_t rows, bool scales, GradPlan* out) {
     try {
         const int64_t wanted = std::max<int64_t>(1, std::min(kGradBlocks / rows, scales ? kGradParts : kGradBlocks));
-        const int64_t most = std::min(grad_parts_per_batch(N, T), wanted), share = ceil_div(T, grad_batches(T));
+        const int64_t most = std::min(grad_parts_per_batch(N, T), wanted);
+        out->strided = false;
+        for (int32_t i = 0; i < T; ++i) out->strided = out->strided || (N > 1 && t[i].stride != t[i].count);
+        const int64_t carries = out->strided ? GradTable<true>::most : GradTable<false>::most, share = ceil_div(T, std::max<int64_t>(1, ceil_div(T, carries)));
         int64_t col = 0;
         out->parts = out->bytes = 0;
         out->batches.clear();
@@ -145,13 +150,14 @@ bool plan_grads(const liec_grad_tensor* t, int32_t T, int32_t N, int64_t rows, b
     return true;
 }
 
-void fill_table(const liec_grad_tensor* t, const GradBatch& g, GradTable* tab) {
+template <bool STRIDED>
+void fill_table(const liec_grad_tensor* t, const GradBatch& g, GradTable<STRIDED>* tab) {
     int64_t col = g.col;
     uint32_t tile = 0;
     for (int32_t i = 0; i < g.count; ++i) {
         const liec_grad_tensor& s = t[g.first + i];
         tab->data[i] = s.data;
-        tab->stride[i] = s.stride;
+        tab->set_stride(i, s.stride);
         tab->col[i] = col;
         tab->first[i] = tile;
         tab->type[i] = (uint8_t)s.dtype;
@@ -176,27 +182,29 @@ GradPass pass_of(const GradCall& c, const GradPlan& plan, const GradBatch& g, bo
     return GradPass{c.partial, sums ? (uint32_t)plan.parts : 0u, slot, (uint32_t)row, (uint32_t)g.tiles, (uint32_t)g.count, c.bound, c.norms, c.rows, c.row_stride};
 }
 
+template <bool STRIDED>
 void launch_squares(const GradCall& c, const GradPlan& plan, int64_t row, int64_t rows, bool stream) {
     uint32_t slot = 0;
-    GradTable tab;
+    GradTable<STRIDED> tab;
     for (const GradBatch& g : plan.batches) {
         fill_table(c.t, g, &tab);
         const GradPass a = pass_of(c, plan, g, true, row, slot);
         const dim3 grid((uint32_t)g.blocks, (uint32_t)rows);
-        if (stream) k_grad_squares<true><<<grid, kBlock, 0, c.st>>>(a, tab);
-        else k_grad_squares<false><<<grid, kBlock, 0, c.st>>>(a, tab);
+        if (stream) k_grad_squares<true, STRIDED><<<grid, kBlock, 0, c.st>>>(a, tab);
+        else k_grad_squares<false, STRIDED><<<grid, kBlock, 0, c.st>>>(a, tab);
         slot += (uint32_t)g.blocks;
     }
 }
 
+template <bool STRIDED>
 void launch_scale(const GradCall& c, const GradPlan& plan, bool sums, int64_t row, int64_t rows) {
-    GradTable tab;
+    GradTable<STRIDED> tab;
     for (const GradBatch& g : plan.batches) {
         fill_table(c.t, g, &tab);
         const GradPass a = pass_of(c, plan, g, sums, row, 0);
         const dim3 grid((uint32_t)g.tiles, (uint32_t)rows);
-        if (c.rows) k_grad_scale<true><<<grid, kBlock, 0, c.st>>>(a, tab);
-        else k_grad_scale<false><<<grid, kBlock, 0, c.st>>>(a, tab);
+        if (c.rows) k_grad_scale<true, STRIDED><<<grid, kBlock, 0, c.st>>>(a, tab);
+        else k_grad_scale<false, STRIDED><<<grid, kBlock, 0, c.st>>>(a, tab);
     }
 }
 
@@ -211,8 +219,8 @@ liec_status run_grads(const GradCall& c) {
         if (!plan_grads(c.t, c.T, c.N, group, scales, &plan)) return LIEC_ENOMEM;
     }
     for (int64_t r = 0; r < N; r += group) {
-        if (sums) launch_squares(c, plan, r, group, !scales);
-        if (scales) launch_scale(c, plan, sums, r, group);
+        if (sums) (plan.strided ? launch_squares<true> : launch_squares<false>)(c, plan, r, group, !scales);
+        if (scales) (plan.strided ? launch_scale<true> : launch_scale<false>)(c, plan, sums, r, group);
     }
     if (c.norms && (!scales || plan.batches.empty())) k_grad_norms<<<(uint32_t)N, kBlock, 0, c.st>>>(c.partial, (uint32_t)plan.parts, c.norms);
     return launched();

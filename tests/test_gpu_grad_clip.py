@@ -65,6 +65,9 @@ COUNTS = {
     "a launch exactly": [5] * 128,
     "a launch and one": [5] * 128 + [40_001],
     "an empty launch": [0] * 128 + [4099],
+    "a launch of contiguous ones": [3] * 183 + [20_000],
+    "and one": [3] * 184 + [20_000],
+    "an empty launch of them": [0] * 184 + [4099],
     "long": [1_000_003, 77, 250_000],
 }
 
@@ -203,6 +206,24 @@ def test_strided_and_shared_tensors():
     wide = torch.randn(4, 200, generator=generator(10), device=DEV)
     pkg.liec_gather_grads([wide[:, 100:160]], wide[:, 20:80])
     assert torch.equal(wide[:, 20:80], wide[:, 100:160])
+
+
+def test_many_columns_of_a_matrix():
+    import paper_2402_11857_amd as pkg
+
+    say("case gradients, 300 columns of a matrix")
+    rows = torch.randn(3, 300 * 41 + 9000, generator=generator(14), device=DEV)
+    views = [rows[:, 41 * i:41 * i + 1 + i % 40] for i in range(300)] + [rows[:, 300 * 41 + 5:]]
+    want = _norms(views, 3)
+    _check_norms(pkg.liec_grad_norm(views), want)
+    before, whole = [v.clone() for v in views], rows.clone()
+    bound = float(want.min()) * 0.7
+    pkg.liec_clip_grads(views, bound)
+    _check_scaled(views, before, _factors(want, bound), 3, "columns")
+    changed = rows != whole
+    for v in views:
+        v.zero_()
+    assert torch.equal(rows != 0, (whole != 0) & ~changed)     # nothing else was touched
 
 
 def test_tensors_of_one_worker_of_any_shape():
