@@ -140,7 +140,7 @@ bool plan_grads(const liec_grad_tensor* t, int32_t T, int32_t N, int64_t rows, b
                 col += t[b + i].count;
             }
             if (!g.tiles) continue;
-            g.blocks = std::min(g.tiles, most);
+            g.blocks = std::min(ceil_div(g.tiles, kGradWaves), most);
             out->parts += g.blocks;
             out->batches.push_back(g);
         }
@@ -202,7 +202,7 @@ void launch_scale(const GradCall& c, const GradPlan& plan, bool sums, int64_t ro
     for (const GradBatch& g : plan.batches) {
         fill_table(c.t, g, &tab);
         const GradPass a = pass_of(c, plan, g, sums, row, 0);
-        const dim3 grid((uint32_t)g.tiles, (uint32_t)rows);
+        const dim3 grid((uint32_t)ceil_div(g.tiles, kGradWaves), (uint32_t)rows);
         if (c.rows) k_grad_scale<true, STRIDED><<<grid, kBlock, 0, c.st>>>(a, tab);
         else k_grad_scale<false, STRIDED><<<grid, kBlock, 0, c.st>>>(a, tab);
     }
