@@ -226,6 +226,29 @@ def test_many_columns_of_a_matrix():
     assert torch.equal(rows != 0, (whole != 0) & ~changed)     # nothing else was touched
 
 
+def test_c_entry_points_with_workers_in_reverse():
+    import ctypes
+
+    import paper_2402_11857_amd as pkg
+    from test_train_abi import Tensor
+
+    say("case gradients through the C entry points, workers in reverse")
+    N, n = 3, 70_001
+    g = torch.randn(N, n, generator=generator(15), device=DEV).bfloat16()
+    want = _norms([g], N)
+    t = Tensor(g.data_ptr() + 2 * (N - 1) * n, n, -n, 1, 0)
+    lib = pkg.lib()
+    need = lib.liec_grads_workspace(N, 1)
+    ws, norms, rows = torch.empty(need, dtype=torch.uint8, device=DEV), torch.empty(N, device=DEV), torch.empty(N, n, device=DEV)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.liec_gather_grads(ctypes.byref(t), 1, N, rows.data_ptr(), n, float("inf"), norms.data_ptr(), ws.data_ptr(), need, stream) == 0
+    _check_norms(norms.flip(0), want)
+    assert torch.equal(rows, g.float().flip(0))
+    before, bound = g.clone(), float(want.min()) / 2
+    assert lib.liec_clip_grads(ctypes.byref(t), 1, N, bound, None, ws.data_ptr(), need, stream) == 0
+    _check_scaled([g], [before], _factors(want, bound), N, "in reverse")
+
+
 def test_tensors_of_one_worker_of_any_shape():
     import paper_2402_11857_amd as pkg
 

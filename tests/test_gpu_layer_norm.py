@@ -326,6 +326,35 @@ def test_another_stream_and_graph_replays():
         assert all(torch.equal(a, c) for a, c in zip((dx, dw, db), want)), f"replay {k}"
 
 
+def test_c_entry_points_without_statistics_and_with_rows_in_reverse():
+    import ctypes
+
+    import paper_2402_11857_amd as pkg
+    from test_train_abi import Param, Rows
+
+    say("case layer norm through the C entry points")
+    lib, ref, N, R = pkg.lib(), ctypes.byref, 2, 7
+    for C in (5, 200, 5000, 17_000):
+        x, _, w, b = _inputs((N, R, C), "fp32", seed=111)
+        y = torch.full((N, R, C), 9.0, device=DEV)
+        # rows from the last to the first, of the last worker first
+        xr = Rows(x.data_ptr() + 4 * (N * R - 1) * C, -R * C, -C)
+        yr = Rows(y.data_ptr() + 4 * (N * R - 1) * C, -R * C, -C)
+        wr, br = Param(w.data_ptr() + 4 * C, -C), Param(b.data_ptr() + 4 * C, -C)
+        stream = torch.cuda.current_stream().cuda_stream
+        assert lib.liec_layer_norm(ref(xr), ref(wr), ref(br), ref(yr), None, None, N, R, C, EPS, 0, 0, stream) == 0
+        want, mean, rstd = pkg.liec_layer_norm(x, w, b, EPS)
+        assert torch.equal(y, want)
+        dw = torch.full((N, C), 9.0, device=DEV)
+        dr = Param(dw.data_ptr() + 4 * C, -C)
+        need = lib.liec_layer_norm_workspace(N, R, C)
+        ws = torch.empty(max(need, 16), dtype=torch.uint8, device=DEV)
+        m, r = mean.flip(0, 1).contiguous(), rstd.flip(0, 1).contiguous()
+        assert lib.liec_layer_norm_backward(ref(xr), ref(xr), m.data_ptr(), r.data_ptr(), ref(wr), None, ref(dr), None, N, R, C, 0, 0,
+                                            ws.data_ptr(), need, stream) == 0
+        _check_backward(x, x, mean, rstd, w, None, dw, None)
+
+
 def test_refusals():
     import paper_2402_11857_amd as pkg
 
