@@ -4,15 +4,16 @@
  * global norm of a worker's gradient tensors, and clipping by it, in place or on the way into the fp32 rows of
  * liec_step.
  *
- * Tensors are DEVICE pointers of one of the types of liec_dtype, at any multiple of the element's size.  The entry points need no context and allocate nothing: they enqueue kernels on
- * `hip_stream` (a hipStream_t passed as void*, NULL = null stream) of the current device and return.  Where scratch
- * is needed the caller passes it (`workspace`, 16-byte aligned DEVICE memory of at least the bytes that the matching
- * *_workspace call names; its contents need no preparation, and calls that may overlap need one each).  They may be
- * captured into a HIP graph.  Argument arrays are HOST memory, read before the call returns.  No entry point throws;
- * every failure is a status code of liec.h (LIEC_EINVAL: nothing was enqueued).
+ * Tensors are DEVICE pointers of one of the types of liec_dtype, at any multiple of the element's size.  The entry
+ * points need no context and allocate nothing: they enqueue kernels on `hip_stream` (a hipStream_t passed as void*,
+ * NULL = null stream) of the current device and return.  Where scratch is needed the caller passes it (`workspace`,
+ * 16-byte aligned DEVICE memory of at least the bytes that the matching ..._workspace call names; its contents need no
+ * preparation, and calls that may overlap need one each).  They may be captured into a HIP graph.  Argument arrays are
+ * HOST memory, read before the call returns.  No entry point throws; every failure is a status code of liec.h
+ * (LIEC_EINVAL: nothing was enqueued).
  *
  * Arithmetic: inputs are widened to fp32 exactly, results are rounded once to the output's type, to nearest; sums of
- * squares of gradients are carried in fp64, the sums of layer normalisation in fp32.  The order of every sum is fixed
+ * squares of gradients are carried in fp64, the sums of layer normalisation in fp32 or more.  The order of every sum is fixed
  * by the sizes, so equal calls give equal bits.
  */
 #ifndef LIEC_TRAIN_H
@@ -99,8 +100,8 @@ typedef struct {
  *   dtype        type of x and y;  param_dtype  type of weight and bias
  *   1 <= N <= 65535, 0 <= R < 2^31 (no rows: nothing to do), 1 <= C <= 2^28, at most 2^40 values, eps >= 0 and
  *                finite; no value lies further than 2^40 values from the first
- * y may be x itself (same pointer and strides); otherwise they must not overlap, and neither may y's rows one another.  Rows of 8 to 16384 columns are read
- * once.
+ * y may be x itself (same pointer and strides); otherwise they must not overlap, and neither may y's rows one
+ * another.  Rows of 8 to 16384 columns are read once.
  */
 liec_status liec_layer_norm(const liec_rows *x, const liec_param *weight, const liec_param *bias, const liec_rows *y,
                             float *mean, float *rstd, int32_t N, int64_t R, int64_t C, float eps, liec_dtype dtype,

@@ -247,9 +247,9 @@ __global__ __launch_bounds__(kLnWide) void k_ln_forward_wide(int64_t C, float ep
 // (2 x C values), or in dw and db themselves where it is the only one (partial == nullptr).  The next P rows of a
 // team are requested ahead.
 template <typename T, int TEAM, int K, bool FULL, int P>
-__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock), (K * Vec16<T>::n == 8 || TEAM == 1024 ? 4 : 2)) void k_ln_backward(uint32_t C, int64_t R, bool keep, float* __restrict__ partial,
-                                                                                const float* __restrict__ mean, const float* __restrict__ rstd, LnRows dy,
-                                                                                LnRows x, LnRows dx, LnParam w, LnParam dw, LnParam db) {
+__global__ __launch_bounds__((TEAM > 64 ? TEAM : kBlock), (K * Vec16<T>::n == 8 || TEAM == 1024 ? 4 : 2))
+void k_ln_backward(uint32_t C, int64_t R, bool keep, float* __restrict__ partial, const float* __restrict__ mean, const float* __restrict__ rstd,
+                   LnRows dy, LnRows x, LnRows dx, LnParam w, LnParam dw, LnParam db) {
     constexpr int TEAMS = TEAM > 64 ? 1 : kBlock / TEAM, WAVES = TEAM > 64 ? TEAM / 64 : 1, V = Vec16<T>::n;
     constexpr int LANES = TEAM > 64 ? 64 : TEAM, COLS = TEAM <= 64 ? TEAM * K * V : 1;
     __shared__ float lds[2][2][WAVES];

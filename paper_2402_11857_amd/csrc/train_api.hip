@@ -360,7 +360,8 @@ void run_forward(const LnForward& a) {
 template <typename T>
 void forward_of(const LnForward& a) {
     if (!holds(a.C)) {
-        k_ln_forward_wide<T><<<dim3((uint32_t)std::min(a.R, kLnWideBlocks), (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.eps, a.R, a.mean, a.rstd, a.x, a.y, a.w, a.b);
+        k_ln_forward_wide<T><<<dim3((uint32_t)std::min(a.R, kLnWideBlocks), (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(
+            a.C, a.eps, a.R, a.mean, a.rstd, a.x, a.y, a.w, a.b);
         return;
     }
     const Team t = forward_team(a.C);
@@ -412,7 +413,8 @@ void backward_of(const LnBackward& a) {
             k_ln_columns_wide<T><<<dim3((uint32_t)ceil_div(a.C, kBlock), (uint32_t)a.N, (uint32_t)a.strips.count), kBlock, 0, a.st>>>(
                 a.C, a.strips.per, a.R, a.partial, a.mean, a.rstd, a.dy, a.x);
         if (a.dx.data)
-            k_ln_backward_wide<T><<<dim3((uint32_t)std::min(a.R, kLnWideBlocks), (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(a.C, a.R, a.mean, a.rstd, a.dy, a.x, a.dx, a.w);
+            k_ln_backward_wide<T><<<dim3((uint32_t)std::min(a.R, kLnWideBlocks), (uint32_t)a.N), a.C < kLnShortest ? 64 : kLnWide, 0, a.st>>>(
+                a.C, a.R, a.mean, a.rstd, a.dy, a.x, a.dx, a.w);
         return;
     }
     const Team t = backward_team(a.C);
