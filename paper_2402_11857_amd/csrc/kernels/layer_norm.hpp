@@ -5,7 +5,8 @@
 //              dw_j = sum over the worker's rows of dy_j h_j,  db_j = sum over them of dy_j
 //
 // A team of TEAM lanes holds one row in registers, K vectors of 16 bytes per lane, so that a row is read once; teams of up
-// to a wave add up inside the wave, larger ones through LDS.  All sums are fp32, of at most a few hundred terms in a chain; rows that no team holds take fp64.
+// to a wave add up inside the wave, larger ones through LDS.  The sums of a row are fp32, in chains of at most 64 additions; a weight
+// gradient is fp32 within a block, over at most 256 rows of a team, and fp64 from there on.  Rows that no team holds take fp64 in all.
 // The last vector of a row that is not a multiple of a vector long starts a vector's length before the row's end: what it
 // shares with the vector before it is left out of the sums and stored twice with the same value, and no access needs a branch.
 //
@@ -404,25 +405,26 @@ void k_ln_backward(uint32_t C, int64_t R, bool keep, float* __restrict__ partial
     }
 }
 
-// dw and db of group blockIdx.y: the sum of its `parts` partial sums, 32 columns per block, 8 threads to a column.
+// dw and db of group blockIdx.y: the sum of its `parts` partial sums, 32 columns per block, 8 threads to a column.  In fp64: the number
+// of parts grows with rows and workers (65535 equal ones in fp32 were off by 1400 u).
 __global__ __launch_bounds__(kBlock) void k_ln_param_grads(const float* __restrict__ partial, uint32_t parts, int64_t C, LnParam dw, LnParam db) {
-    __shared__ float lds[8][32];
+    __shared__ double lds[8][32];
     const LnParam& out = blockIdx.z ? db : dw;
     if (!out.data) return;
     const uint32_t col = threadIdx.x & 31, slice = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + col;
     const float* const p = partial + (size_t)blockIdx.y * parts * 2 * C + (blockIdx.z ? C : 0);
-    float s = 0.f;
+    double s = 0.0;
     if (c < C) {
 #pragma unroll 4
-        for (uint32_t q = slice; q < parts; q += 8) s += p[(size_t)q * 2 * C + c];
+        for (uint32_t q = slice; q < parts; q += 8) s += (double)p[(size_t)q * 2 * C + c];
     }
     lds[slice][col] = s;
     __syncthreads();
     if (slice == 0 && c < C) {
         s = lds[0][col];
         for (int q = 1; q < 8; ++q) s += lds[q][col];
-        store_any(out.data, (int64_t)blockIdx.y * out.stride + c, out.type, s);
+        store_any(out.data, (int64_t)blockIdx.y * out.stride + c, out.type, (float)s);
     }
 }
 
@@ -460,7 +462,7 @@ __global__ __launch_bounds__(kLnWide) void k_ln_backward_wide(int64_t C, int64_t
     }
 }
 
-// The same rows' share of dw and db: block (columns, worker, strip), a thread to a column.
+// The same rows' share of dw and db: block (columns, worker, strip), a thread to a column.  In fp64: a strip may have any number of rows.
 template <typename T>
 __global__ __launch_bounds__(kBlock) void k_ln_columns_wide(int64_t C, int64_t per, int64_t R, float* __restrict__ partial, const float* __restrict__ mean,
                                                             const float* __restrict__ rstd, LnRows dy, LnRows x) {
@@ -470,16 +472,16 @@ __global__ __launch_bounds__(kBlock) void k_ln_columns_wide(int64_t C, int64_t p
     const int64_t begin = (int64_t)strip * per, end = min(begin + per, R);
     const T* const xs = static_cast<const T*>(x.data) + (int64_t)worker * x.worker + c;
     const T* const gs = static_cast<const T*>(dy.data) + (int64_t)worker * dy.worker + c;
-    float aw = 0.f, ab = 0.f;
+    double aw = 0.0, ab = 0.0;
 #pragma unroll 4
     for (int64_t r = begin; r < end; ++r) {
         const float mu = mean[(int64_t)worker * R + r], rs = rstd[(int64_t)worker * R + r], g = widen(gs[r * dy.row]);
-        ab += g;
-        aw = __fmaf_rn(g, (widen(xs[r * x.row]) - mu) * rs, aw);
+        ab += (double)g;
+        aw = __fma_rn((double)g, (double)((widen(xs[r * x.row]) - mu) * rs), aw);
     }
     float* const out = partial + ((size_t)worker * gridDim.z + strip) * 2 * C;
-    out[c] = aw;
-    out[C + c] = ab;
+    out[c] = (float)aw;
+    out[C + c] = (float)ab;
 }
 
 }  // namespace liec

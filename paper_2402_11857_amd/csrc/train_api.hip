@@ -277,7 +277,9 @@ Strips strips_of(int32_t N, int64_t R, const Team& t, int64_t waves) {
 // Strips of the backward pass, each with partial sums of its own: as many blocks as are resident at a time.  Weight gradients
 // stay in registers; one vector per lane leaves room for four waves (six: as fast or 2 to 30 % slower); of two per lane two
 // waves that request two rows ahead beat four that request one (2048 columns 156 against 166 us, 8192 286 against 299); 16
-// waves to a row are four by themselves.
+// waves to a row are four by themselves.  A team adds up at most kLnChain rows in fp32; where that takes more blocks, they are a
+// multiple of those that are resident.
+constexpr int64_t kLnChain = 256;
 Strips backward_strips(int32_t N, int64_t R, int64_t C) {
     if (R == 0) return {1, 0};
     if (!holds(C)) {                   // the columns' sums, a thread per column
@@ -287,7 +289,11 @@ Strips backward_strips(int32_t N, int64_t R, int64_t C) {
     const Team t = backward_team(C);
     // few rows: one block, whose sums need no second kernel
     if (R <= 8 * teams_of(t)) return {R, 1};
-    return strips_of(N, R, t, t.eights == 1 || t.lanes == 1024 ? 4 : 2);
+    const Strips s = strips_of(N, R, t, t.eights == 1 || t.lanes == 1024 ? 4 : 2);
+    const int64_t rounds = ceil_div(s.per, kLnChain * teams_of(t));
+    if (rounds == 1) return s;
+    const int64_t per = ceil_div(R, s.count * rounds);
+    return {per, ceil_div(R, per)};
 }
 
 constexpr int64_t kMostValues = (int64_t)1 << 40;
