@@ -5,6 +5,7 @@
 // and strides ValueError, what the library refuses its own error class; no C++ exception leaves a function.
 #include <torch/extension.h>
 
+#include <algorithm>
 #include <new>
 #include <string>
 #include <vector>
@@ -198,10 +199,34 @@ PyObject* gather_grads(PyObject* const* a) {   // grads, rows, max_norm, norms, 
 // ---- layer normalisation ---------------------------------------------------------------------------------------------
 struct Sizes {
     int64_t N, R, C;
+    int64_t split;                     // dimensions before this one are the workers', those from it up to the columns the rows'
 };
 
-// Workers, rows of each and columns of activations x under these weights, biases and their gradients (some of them nullptr).
-Sizes sizes_of(const at::Tensor& x, std::initializer_list<const at::Tensor*> params) {
+// The distance of dimensions [from, to) of t seen as one; false where they are not evenly spaced.
+bool merged(const at::Tensor& t, int64_t from, int64_t to, int64_t* stride) {
+    int64_t next = -1;                 // what the next dimension's distance has to be; -1: any
+    *stride = 0;
+    for (int64_t d = to - 1; d >= from; --d) {
+        if (t.size(d) == 1) continue;
+        if (next < 0) *stride = t.stride(d);
+        else if (t.stride(d) != next) return false;
+        next = t.stride(d) * t.size(d);
+    }
+    return true;
+}
+
+// t as workers' rows; false where no two distances describe it.
+bool as_rows(const at::Tensor& t, const Sizes& s, liec_rows* r) {
+    r->data = t.data_ptr();
+    r->worker_stride = s.R * s.C;
+    r->row_stride = s.C;
+    if (t.is_contiguous()) return true;
+    return merged(t, 0, s.split, &r->worker_stride) && merged(t, s.split, t.dim() - 1, &r->row_stride);
+}
+
+// Workers, rows of each and columns of activations x under these weights, biases and their gradients (some of them nullptr).  Where
+// none of them has rows for the workers any split of the dimensions will do: the first that all operands are laid out for.
+Sizes sizes_of(const at::Tensor& x, std::initializer_list<const at::Tensor*> params, std::initializer_list<const at::Tensor*> operands) {
     const int64_t dims = x.dim(), C = dims ? x.size(-1) : 0;
     if (C < 1) value_error("activations of shape " + text(x.sizes()) + " have no columns");
     int64_t N = 0;
@@ -214,21 +239,25 @@ Sizes sizes_of(const at::Tensor& x, std::initializer_list<const at::Tensor*> par
             if (dims < 2 || N != x.size(0) || !N) value_error("weights of " + std::to_string(N) + " workers do not fit activations of shape " + text(x.sizes()));
         }
     }
-    if (N) return {N, x.numel() / (N * C), C};
-    if (dims == 3 && x.size(0) && !x.is_contiguous()) return {x.size(0), x.size(1), C};
-    return {1, x.numel() / C, C};
+    const int64_t rows = x.numel() / C;
+    if (N) return {N, rows / N, C, 1};
+    N = 1;
+    for (int64_t split = 0; rows && split < std::max<int64_t>(1, dims - 1); N *= x.size(split++)) {
+        const Sizes s{N, rows / N, C, split};
+        bool all = N <= 65535;
+        liec_rows r;
+        for (const at::Tensor* t : operands) all = all && (!t || as_rows(*t, s, &r));
+        if (all) return s;
+    }
+    return {1, rows, C, 0};
 }
 
 liec_rows rows_of(const at::Tensor& t, const Sizes& s, const char* what) {
-    if (t.is_contiguous()) return {t.data_ptr(), s.R * s.C, s.C};
-    at::Tensor v;
-    try {
-        v = t.view({s.N, s.R, s.C});
-    } catch (const c10::Error&) {
+    if (s.C > 1 && t.stride(-1) != 1 && !t.is_contiguous()) value_error(std::string("the columns of ") + what + " must be contiguous");
+    liec_rows r;
+    if (!as_rows(t, s, &r))
         value_error(std::string(what) + " of strides " + text(t.strides()) + " is not " + std::to_string(s.N) + " workers' rows at equal distances");
-    }
-    if (s.C > 1 && v.stride(2) != 1) value_error(std::string("the columns of ") + what + " must be contiguous");
-    return {t.data_ptr(), v.stride(0), v.stride(1)};
+    return r;
 }
 
 void check_like(const at::Tensor& t, const at::Tensor& x, const char* what) {
@@ -267,8 +296,8 @@ PyObject* layer_norm(PyObject* const* a) {     // x, weight, bias, eps, out
     const at::Tensor *weight = optional_tensor(a[1], "weight"), *bias = optional_tensor(a[2], "bias"), *out = optional_tensor(a[4], "out");
     const double eps = number(a[3]);
     const int code = activations_code(x), pcode = params_code(x, {weight, bias});
-    const Sizes s = sizes_of(x, {weight, bias});
     if (out) check_like(*out, x, "out");
+    const Sizes s = sizes_of(x, {weight, bias}, {&x, out});
     const at::Tensor y = out ? *out : new_tensor(x.sizes(), x.scalar_type(), x);
     const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
     const at::Tensor mean = new_tensor(lead, at::kFloat, x), rstd = new_tensor(lead, at::kFloat, x);
@@ -297,11 +326,9 @@ PyObject* layer_norm_backward(PyObject* const* a) {   // dy, x, mean, rstd, weig
     const bool need = a[8] == Py_True;
     const at::Tensor* const given = need ? optional_tensor(a[5], "dx") : nullptr;
     const int code = activations_code(x), pcode = params_code(x, {weight, dweight, dbias});
-    Sizes s = sizes_of(x, {weight, dweight, dbias});
     check_like(dy, x, "dy");
     if (given) check_like(*given, x, "dx");
-    // one weight for all: any split of the rows will do
-    if (s.N == 1 && x.dim() == 3 && x.size(0) && !(dy.is_contiguous() && (!given || given->is_contiguous()))) s = {x.size(0), x.size(1), s.C};
+    const Sizes s = sizes_of(x, {weight, dweight, dbias}, {&x, &dy, given});
     const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
     for (const at::Tensor* t : {&mean, &rstd})
         if (t->scalar_type() != at::kFloat || t->device() != x.device() || t->sizes() != lead || !t->is_contiguous())
