@@ -278,6 +278,12 @@ int params_code(const at::Tensor& x, std::initializer_list<const at::Tensor*> pa
     return code < 0 ? (int)LIEC_F32 : code;
 }
 
+// Gradients with a row for each worker need room for each: one vector seen N times would hold the sum over all of them.
+void check_rows_apart(const at::Tensor* p, const char* what) {
+    if (p && p->dim() == 2 && p->size(0) > 1 && p->stride(0) == 0)
+        value_error(std::string(what) + " is an expanded tensor, which cannot hold a sum for each worker: pass one vector for the sum over all of them");
+}
+
 liec_param param_of(const at::Tensor* p) { return p ? liec_param{p->data_ptr(), p->dim() == 2 ? p->stride(0) : 0} : liec_param{nullptr, 0}; }
 
 int activations_code(const at::Tensor& x) {
@@ -329,6 +335,8 @@ PyObject* layer_norm_backward(PyObject* const* a) {   // dy, x, mean, rstd, weig
     check_like(dy, x, "dy");
     if (given) check_like(*given, x, "dx");
     const Sizes s = sizes_of(x, {weight, dweight, dbias}, {&x, &dy, given});
+    check_rows_apart(dweight, "dweight");
+    check_rows_apart(dbias, "dbias");
     const at::IntArrayRef lead = x.sizes().slice(0, x.dim() - 1);
     for (const at::Tensor* t : {&mean, &rstd})
         if (t->scalar_type() != at::kFloat || t->device() != x.device() || t->sizes() != lead || !t->is_contiguous())
