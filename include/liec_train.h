@@ -65,7 +65,8 @@ liec_status liec_grad_norm(const liec_grad_tensor *tensors, int32_t T, int32_t N
  *   max_norm  >= 0, not NaN
  *   norms     NULL, or N fp32 values (DEVICE): the norms before clipping
  * No two tensors, nor two workers' values of one, may share memory (LIEC_EINVAL, for instance for a tied tensor that
- * is listed twice).
+ * is listed twice).  They may lie between one another where their strides are equal or opposite in bytes, such as
+ * columns of a matrix; tensors that do so at strides that differ count as sharing.
  */
 liec_status liec_clip_grads(const liec_grad_tensor *tensors, int32_t T, int32_t N, float max_norm, float *norms,
                             void *workspace, int64_t workspace_bytes, void *hip_stream);
@@ -73,7 +74,8 @@ liec_status liec_clip_grads(const liec_grad_tensor *tensors, int32_t T, int32_t 
 /*
  * liec_gather_grads: the tensors, clipped as by liec_clip_grads, one after the other into the fp32 rows that
  * liec_step reads: worker i's values of tensor t go to rows + i * row_stride + (counts of the tensors before t).
- * The tensors are read only (any stride); a tensor that shares memory with the rows is LIEC_EINVAL.
+ * The tensors are read only (any stride); a tensor that shares memory with the rows is LIEC_EINVAL.  At strides that
+ * differ from the rows', more than 2^22 workers' values that lie between the rows count as sharing.
  *   row_stride  >= the sum of the counts
  *   max_norm = +Inf with norms = NULL only gathers: one kernel for up to 128 tensors, each value read once.
  */

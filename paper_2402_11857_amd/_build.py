@@ -9,7 +9,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 LIB_PATH = os.path.join(_HERE, "libliec.so")
 SOURCES = [os.path.join(_HERE, "csrc", n) for n in ("liec_api.hip", "train_api.hip")]
-HEADERS = [os.path.join(_HERE, "csrc", "liec_kernels.hpp"), os.path.join(_ROOT, "include", "liec.h"),
+HEADERS = [os.path.join(_HERE, "csrc", "liec_kernels.hpp"), os.path.join(_HERE, "csrc", "spans.hpp"), os.path.join(_ROOT, "include", "liec.h"),
            os.path.join(_ROOT, "include", "liec_testing.h"), os.path.join(_ROOT, "include", "liec_train.h")] + \
           [os.path.join(_HERE, "csrc", "kernels", n)
            for n in ("common.hpp", "elements.hpp", "grads.hpp", "layer_norm.hpp", "rows.hpp", "select.hpp", "sign.hpp", "step.hpp", "sync.hpp",

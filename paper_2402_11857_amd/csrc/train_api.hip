@@ -11,6 +11,7 @@
 
 #include "kernels/grads.hpp"
 #include "kernels/layer_norm.hpp"
+#include "spans.hpp"
 
 using namespace liec;
 
@@ -60,53 +61,21 @@ bool valid_grads(const liec_grad_tensor* t, int32_t T, int32_t N, int64_t* total
 
 bool valid_workspace(const void* ws, int64_t bytes, int64_t need) { return ws && aligned_to(ws, 16) && bytes >= need; }
 
-// Do two sets of N equally spaced byte ranges (first starts, lengths, distances) share a byte?
-bool ranges_meet(uintptr_t a, int64_t an, int64_t as, uintptr_t b, int64_t bn, int64_t bs, int32_t N) {
-    if (an <= 0 || bn <= 0) return false;
-    const int64_t last = N - 1, d = (int64_t)(b - a);
-    const int64_t alo = std::min<int64_t>(0, as * last), ahi = std::max<int64_t>(0, as * last) + an;
-    const int64_t blo = d + std::min<int64_t>(0, bs * last), bhi = d + std::max<int64_t>(0, bs * last) + bn;
-    if (bhi <= alo || ahi <= blo) return false;
-    if (as != bs || N == 1 || as <= 0) return true;
-    // the same distance: columns of one matrix.  Range i of b lies d + (i - j) * as from range j of a.
-    int64_t off = d % as;
-    if (off < 0) off += as;
-    const int64_t row = (d - off) / as;                        // b's range i is off bytes into a's row i + row
-    return (off < an && row <= last && row >= -last) || (off + bn > as && row + 1 <= last && row + 1 >= -last);
+// Where worker 0's values to worker N - 1's of a tensor lie.
+Span span_of_grads(const liec_grad_tensor& t, int32_t N) {
+    const int64_t size = size_of(t.dtype);
+    return span_of(t.data, t.count * size, t.stride * size, N);
 }
 
 // Do any two tensors, or two workers' values of one, share memory?  May throw std::bad_alloc.
 bool grads_meet(const liec_grad_tensor* t, int32_t T, int32_t N) {
-    struct Range {
-        uintptr_t first, lo, hi;              // worker 0's start; where the values of all workers lie
-        int64_t bytes, stride;
-    };
-    std::vector<Range> all;
+    std::vector<Span> all;
     all.reserve((size_t)T);
-    bool matrix = N > 1;                      // columns of one matrix of N rows
     for (int32_t i = 0; i < T; ++i) {
-        if (!t[i].count) continue;
-        if (N > 1 && llabs(t[i].stride) < t[i].count) return true;
-        const int64_t size = size_of(t[i].dtype), stride = N > 1 ? t[i].stride * size : 0, reach = stride * (N - 1);
-        const uintptr_t p = (uintptr_t)t[i].data;
-        all.push_back({p, p + (uintptr_t)std::min<int64_t>(0, reach), p + (uintptr_t)(std::max<int64_t>(0, reach) + t[i].count * size), t[i].count * size, stride});
-        matrix = matrix && stride > 0 && stride == all[0].stride;
+        if (t[i].count && N > 1 && llabs(t[i].stride) < t[i].count) return true;
+        all.push_back(span_of_grads(t[i], N));
     }
-    std::sort(all.begin(), all.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
-    // starts and ends within one row of the matrix: neighbours are all there is to compare
-    matrix = matrix && !all.empty() && all.back().first - all[0].first < (uintptr_t)all[0].stride;
-    for (const Range& r : all) matrix = matrix && r.first + (uintptr_t)r.bytes <= all[0].first + (uintptr_t)all[0].stride;
-    uintptr_t reached = 0;                    // by the tensors before
-    for (size_t i = 0; i < all.size(); ++i) {
-        if (matrix) {
-            if (i && all[i].first < all[i - 1].first + (uintptr_t)all[i - 1].bytes) return true;
-            continue;
-        }
-        for (size_t j = 0; j < i && all[i].lo < reached; ++j)
-            if (all[j].hi > all[i].lo && ranges_meet(all[j].first, all[j].bytes, all[j].stride, all[i].first, all[i].bytes, all[i].stride, N)) return true;
-        reached = std::max(reached, all[i].hi);
-    }
-    return false;
+    return any_meet(all);
 }
 
 struct GradBatch {
@@ -474,11 +443,10 @@ liec_status liec_gather_grads(const liec_grad_tensor* tensors, int32_t T, int32_
     if (total && (!rows || !aligned_to(rows, 4))) return LIEC_EINVAL;
     if (N > 1 && (row_stride < total || row_stride > kMaxGradValues)) return LIEC_EINVAL;
     if (!valid_workspace(workspace, workspace_bytes, liec_grads_workspace(N, T))) return LIEC_EINVAL;
-    for (int32_t i = 0; i < T; ++i) {
-        const int64_t s = size_of(tensors[i].dtype);
-        if (ranges_meet((uintptr_t)rows, total * 4, row_stride * 4, (uintptr_t)tensors[i].data, tensors[i].count * s, tensors[i].stride * s, N))
-            return LIEC_EINVAL;
-    }
+    const Span written = span_of(rows, total * 4, N > 1 ? row_stride * 4 : 0, N);
+    int64_t steps = kSpanSteps;
+    for (int32_t i = 0; i < T; ++i)
+        if (spans_meet(written, span_of_grads(tensors[i], N), steps)) return LIEC_EINVAL;
     return run_grads(GradCall{tensors, T, N, rows, row_stride, max_norm, norms, static_cast<double*>(workspace), (hipStream_t)hip_stream});
 }
 
