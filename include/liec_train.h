@@ -8,9 +8,9 @@
  * points need no context and allocate nothing: they enqueue kernels on `hip_stream` (a hipStream_t passed as void*,
  * NULL = null stream) of the current device and return.  Where scratch is needed the caller passes it (`workspace`,
  * 16-byte aligned DEVICE memory of at least the bytes that the matching ..._workspace call names; its contents need no
- * preparation, and calls that may overlap need one each).  They may be captured into a HIP graph.  Argument arrays are
- * HOST memory, read before the call returns.  No entry point throws; every failure is a status code of liec.h
- * (LIEC_EINVAL: nothing was enqueued).
+ * preparation, it shares no memory with the call's other arguments, and calls that may overlap need one each).  They may
+ * be captured into a HIP graph.  Argument arrays are HOST memory, read before the call returns.  No entry point throws;
+ * every failure is a status code of liec.h (LIEC_EINVAL: nothing was enqueued).
  *
  * Arithmetic: inputs are widened to fp32 exactly, results are rounded once to the output's type, to nearest; sums of
  * squares of gradients are carried in fp64, the sums of layer normalisation in fp32 or more.  The order of every sum is fixed
@@ -63,7 +63,7 @@ liec_status liec_grad_norm(const liec_grad_tensor *tensors, int32_t T, int32_t N
  * A worker whose norm is NaN gets NaN everywhere, one whose norm is infinite gets zeros and NaN; max_norm = +Inf
  * clips nothing.
  *   max_norm  >= 0, not NaN
- *   norms     NULL, or N fp32 values (DEVICE): the norms before clipping
+ *   norms     NULL, or N fp32 values (DEVICE) outside the tensors: the norms before clipping
  * No two tensors, nor two workers' values of one, may share memory (LIEC_EINVAL, for instance for a tied tensor that
  * is listed twice).  They may lie between one another where their strides are equal or opposite in bytes, such as
  * columns of a matrix; tensors that do so at strides that differ count as sharing.
@@ -74,7 +74,8 @@ liec_status liec_clip_grads(const liec_grad_tensor *tensors, int32_t T, int32_t 
 /*
  * liec_gather_grads: the tensors, clipped as by liec_clip_grads, one after the other into the fp32 rows that
  * liec_step reads: worker i's values of tensor t go to rows + i * row_stride + (counts of the tensors before t).
- * The tensors are read only (any stride); a tensor that shares memory with the rows is LIEC_EINVAL.  At strides that
+ * The tensors are read only (any stride); a tensor that shares memory with the rows or the norms is LIEC_EINVAL, and
+ * so are norms in the rows.  At strides that
  * differ from the rows', more than 2^22 workers' values that lie between the rows count as sharing.
  *   row_stride  >= the sum of the counts
  *   max_norm = +Inf with norms = NULL only gathers: one kernel for up to 128 tensors, each value read once.

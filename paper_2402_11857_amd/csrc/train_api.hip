@@ -78,6 +78,18 @@ bool grads_meet(const liec_grad_tensor* t, int32_t T, int32_t N) {
     return any_meet(all);
 }
 
+// The norms of N workers and the partial sums are written while other blocks read the gradients, and the norms while others read
+// the partial sums.  `after`: the norms come from a launch of their own, when the gradients have been read.
+bool grads_apart_from(const liec_grad_tensor* t, int32_t T, int32_t N, const float* norms, bool after, const void* workspace) {
+    const Span n = span_of(norms, (int64_t)N * 4), ws = span_of(workspace, liec_grads_workspace(N, T));
+    if (span_meets(ws, n.lo, n.hi)) return false;
+    for (int32_t i = 0; i < T; ++i) {
+        const Span g = span_of_grads(t[i], N);
+        if ((!after && span_meets(g, n.lo, n.hi)) || span_meets(g, ws.lo, ws.hi)) return false;
+    }
+    return true;
+}
+
 struct GradBatch {
     int32_t first, count;
     int64_t tiles, blocks, col;               // col: column of its first tensor
@@ -420,6 +432,7 @@ liec_status liec_grad_norm(const liec_grad_tensor* tensors, int32_t T, int32_t N
     int64_t total = 0;
     if (!valid_grads(tensors, T, N, &total) || !norms || !aligned_to(norms, 4)) return LIEC_EINVAL;
     if (!valid_workspace(workspace, workspace_bytes, liec_grads_workspace(N, T))) return LIEC_EINVAL;
+    if (!grads_apart_from(tensors, T, N, norms, true, workspace)) return LIEC_EINVAL;
     return run_grads(GradCall{tensors, T, N, nullptr, 0, INFINITY, norms, static_cast<double*>(workspace), (hipStream_t)hip_stream});
 }
 
@@ -428,6 +441,7 @@ liec_status liec_clip_grads(const liec_grad_tensor* tensors, int32_t T, int32_t 
     int64_t total = 0;
     if (!valid_grads(tensors, T, N, &total) || !aligned_to(norms, 4) || !(max_norm >= 0.f)) return LIEC_EINVAL;
     if (!valid_workspace(workspace, workspace_bytes, liec_grads_workspace(N, T))) return LIEC_EINVAL;
+    if (!grads_apart_from(tensors, T, N, norms, false, workspace)) return LIEC_EINVAL;
     try {
         if (grads_meet(tensors, T, N)) return LIEC_EINVAL;
     } catch (const std::bad_alloc&) {
@@ -444,6 +458,11 @@ liec_status liec_gather_grads(const liec_grad_tensor* tensors, int32_t T, int32_
     if (N > 1 && (row_stride < total || row_stride > kMaxGradValues)) return LIEC_EINVAL;
     if (!valid_workspace(workspace, workspace_bytes, liec_grads_workspace(N, T))) return LIEC_EINVAL;
     const Span written = span_of(rows, total * 4, N > 1 ? row_stride * 4 : 0, N);
+    if (norms || max_norm < INFINITY) {
+        const Span n = span_of(norms, (int64_t)N * 4), ws = span_of(workspace, liec_grads_workspace(N, T));
+        if (!grads_apart_from(tensors, T, N, norms, false, workspace) || span_meets(written, n.lo, n.hi) || span_meets(written, ws.lo, ws.hi))
+            return LIEC_EINVAL;
+    }
     int64_t steps = kSpanSteps;
     for (int32_t i = 0; i < T; ++i)
         if (spans_meet(written, span_of_grads(tensors[i], N), steps)) return LIEC_EINVAL;
