@@ -104,7 +104,8 @@ typedef struct {
  *   1 <= N <= 65535, 0 <= R < 2^31 (no rows: nothing to do), 1 <= C <= 2^28, at most 2^40 values, eps >= 0 and
  *                finite; no value lies further than 2^40 values from the first
  * y may be x itself (same pointer and strides); otherwise they must not overlap, and neither may y's rows one
- * another.  Rows of 8 to 16384 columns are read once.
+ * another (LIEC_EINVAL; at strides that differ, more than 2^22 rows of both that lie between one another count as
+ * overlapping).  Rows of 8 to 16384 columns are read once.
  */
 liec_status liec_layer_norm(const liec_rows *x, const liec_param *weight, const liec_param *bias, const liec_rows *y,
                             float *mean, float *rstd, int32_t N, int64_t R, int64_t C, float eps, liec_dtype dtype,
@@ -119,8 +120,8 @@ int64_t liec_layer_norm_workspace(int32_t N, int64_t R, int64_t C);
  *   dx = rstd * (a - mean(a) - h * mean(a h)),  dweight_i = sum over worker i's rows of dy * h,  dbias_i of dy.
  * dweight and dbias with stride 0 take the sum over all workers' rows.  They are written, not added to, also where
  * there are no rows (zeros).
- *   dx           NULL, or data = NULL, where it is not asked for; dx may be dy or x itself (same pointer and strides);
- *                its rows must not overlap
+ *   dx           NULL, or data = NULL, where it is not asked for; dx may be dy or x itself (same pointer and strides),
+ *                as for liec_layer_norm; its rows must not overlap
  *   mean, rstd   as liec_layer_norm left them
  *   param_dtype  type of weight, dweight and dbias
  */

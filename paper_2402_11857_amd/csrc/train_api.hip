@@ -293,19 +293,15 @@ bool apart(const liec_rows* r, int32_t N, int64_t R, int64_t C) {
     }
     return (n == 1 || s >= C) && (many == 1 || wide >= (n - 1) * s + C);
 }
-bool same(const liec_rows* a, const liec_rows* b) {
-    return a->data == b->data && a->worker_stride == b->worker_stride && a->row_stride == b->row_stride;
+bool same(const liec_rows* a, const liec_rows* b, int32_t N, int64_t R) {
+    return a->data == b->data && (N == 1 || a->worker_stride == b->worker_stride) && (R == 1 || a->row_stride == b->row_stride);
 }
-bool dense(const liec_rows* a, int32_t N, int64_t R, int64_t C) {
-    return (R == 1 || a->row_stride == C) && (N == 1 || a->worker_stride == R * C);
+Span span_of_rows(const liec_rows* r, int32_t N, int64_t R, int64_t C, int64_t size) {
+    return span_of(r->data, C * size, r->row_stride * size, R, r->worker_stride * size, N);
 }
-// An output may be an input, and must not share memory with it otherwise; what is not dense can be told apart by its start only.
+// An output may be an input, and must not share memory with it otherwise.
 bool may_write(const liec_rows* out, const liec_rows* in, int32_t N, int64_t R, int64_t C, int64_t size) {
-    if (same(out, in)) return true;
-    if (out->data == in->data) return false;
-    if (!dense(out, N, R, C) || !dense(in, N, R, C)) return true;
-    const uintptr_t a = (uintptr_t)out->data, b = (uintptr_t)in->data, bytes = (uintptr_t)(N * R * C * size);
-    return a + bytes <= b || b + bytes <= a;
+    return same(out, in, N, R) || !spans_meet(span_of_rows(out, N, R, C, size), span_of_rows(in, N, R, C, size));
 }
 LnRows rows_of(const liec_rows* r) { return r ? LnRows{r->data, r->worker_stride, r->row_stride} : LnRows{nullptr, 0, 0}; }
 LnParam param_of(const liec_param* p, int type) { return p && p->data ? LnParam{p->data, p->stride, (uint32_t)type} : LnParam{nullptr, 0, (uint32_t)type}; }

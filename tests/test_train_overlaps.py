@@ -7,7 +7,7 @@ import sys
 import pytest
 
 sys.path.insert(0, os.path.dirname(__file__))
-from test_train_abi import Tensor, lib  # noqa: E402,F401
+from test_train_abi import Param, Rows, Tensor, lib  # noqa: E402,F401
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="passes addresses that no memory stands behind")
@@ -50,3 +50,54 @@ def test_norms_and_scratch_of_the_gradient_operators(lib):  # noqa: F811
     assert not refused("gather", rows + 4 * 1077, ws)        # between the first two
     assert refused("gather", norms, rows + 16)               # scratch in the rows
     assert not refused("gather", None, rows + 16, bound=float("inf"))     # scratch that is not used
+
+
+class _LayerNorm:
+    """Calls on fp32 operands of N x R rows of C columns, each at an address of its own unless one is given."""
+
+    def __init__(self, lib, N, R, C):  # noqa: F811
+        self.lib, self.N, self.R, self.C = lib, N, R, C
+        self.need = lib.liec_layer_norm_workspace(N, R, C)
+
+    def rows(self, k):
+        return Rows(k * MB, self.R * self.C, self.C)
+
+    def forward(self, x=None, y=None, w=None, b=None, mean=7 * MB, rstd=8 * MB):
+        ref, x, y = ctypes.byref, x or self.rows(1), y or self.rows(2)
+        w, b = w or Param(5 * MB, self.C), b or Param(6 * MB, self.C)
+        return self.lib.liec_layer_norm(ref(x), ref(w), ref(b), ref(y), mean, rstd, self.N, self.R, self.C, 1e-5, 0, 0, None)
+
+    def backward(self, dy=None, x=None, dx=None, w=None, dw=None, db=None, mean=7 * MB, rstd=8 * MB, ws=11 * MB, ptype=0):
+        ref, dy, x, dx = ctypes.byref, dy or self.rows(1), x or self.rows(2), dx or self.rows(3)
+        w, dw, db = w or Param(5 * MB, self.C), dw or Param(9 * MB, self.C), db or Param(10 * MB, self.C)
+        return self.lib.liec_layer_norm_backward(ref(dy), ref(x), mean, rstd, ref(w), ref(dx), ref(dw), ref(db), self.N, self.R, self.C, 0, ptype, ws,
+                                                 self.need, None)
+
+
+def test_rows_that_are_written_and_rows_that_are_read(lib):  # noqa: F811
+    N, R, C, S = 3, 10, 64, 200
+    f = _LayerNorm(lib, N, R, C)
+    assert f.forward() != EINVAL and f.backward() != EINVAL
+
+    def wide(column, row=0, s=S):                            # columns of a matrix of s values a row
+        return Rows(12 * MB + 4 * (row * s + column), R * s, s)
+
+    for a, b, meet in ((wide(0), wide(64), False), (wide(0), wide(63), True), (wide(64), wide(0), False), (wide(3), wide(0), True),
+                       (wide(0, 1), wide(0), True), (wide(0, 1), wide(64), False), (wide(0, 1), wide(137), True), (wide(0, 1), wide(136), False),
+                       (wide(0, N * R), wide(0), False), (wide(0, N * R - 1), wide(0), True),
+                       (wide(0), Rows(12 * MB + 4 * 64, R * S + S, S), False),               # one distance differs
+                       (wide(0), Rows(12 * MB + 4 * 64, R * S + S - 1, S), True),
+                       (wide(0), Rows(12 * MB + 4 * 64, R * S, 2 * S), False),               # rows of a worker reach the next one's
+                       (wide(0), Rows(12 * MB + 4 * 64, 2 * R * S, 2 * S), False),
+                       (wide(0), Rows(12 * MB + 4 * 64, 2 * R * S, 2 * S + 30), True),
+                       (wide(0), Rows(12 * MB + 4 * ((N * R - 1) * S), -R * S, -S), True),   # the same rows in reverse
+                       (wide(0), Rows(12 * MB + 4 * ((N * R - 1) * S + 64), -R * S, -S), False)):
+        assert (f.forward(x=b, y=a) == EINVAL) == meet
+        assert (f.backward(dy=b, dx=a) == EINVAL) == meet
+        assert (f.backward(x=b, dx=a) == EINVAL) == meet
+    # in place, with distances that nothing is counted with
+    one = _LayerNorm(lib, 1, R, C)
+    assert one.forward(x=Rows(MB, 0, S), y=Rows(MB, 77, S)) != EINVAL
+    assert one.forward(x=Rows(MB, 0, S), y=Rows(MB, 0, S + 1)) == EINVAL
+    row = _LayerNorm(lib, N, 1, C)
+    assert row.backward(dy=Rows(MB, S, 0), dx=Rows(MB, S, 5)) != EINVAL
