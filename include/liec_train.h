@@ -119,7 +119,8 @@ int64_t liec_layer_norm_workspace(int32_t N, int64_t R, int64_t C);
  * liec_layer_norm_backward: with h = (x - mean) * rstd and a = dy * weight,
  *   dx = rstd * (a - mean(a) - h * mean(a h)),  dweight_i = sum over worker i's rows of dy * h,  dbias_i of dy.
  * dweight and dbias with stride 0 take the sum over all workers' rows.  They are written, not added to, also where
- * there are no rows (zeros).
+ * there are no rows (zeros).  They share no memory with each other or with other operands; either may take the place
+ * of weight itself (same pointer and stride).
  *   dx           NULL, or data = NULL, where it is not asked for; dx may be dy or x itself (same pointer and strides),
  *                as for liec_layer_norm; its rows must not overlap
  *   mean, rstd   as liec_layer_norm left them

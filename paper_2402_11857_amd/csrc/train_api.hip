@@ -303,6 +303,14 @@ Span span_of_rows(const liec_rows* r, int32_t N, int64_t R, int64_t C, int64_t s
 bool may_write(const liec_rows* out, const liec_rows* in, int32_t N, int64_t R, int64_t C, int64_t size) {
     return same(out, in, N, R) || !spans_meet(span_of_rows(out, N, R, C, size), span_of_rows(in, N, R, C, size));
 }
+Span span_of_param(const liec_param* p, int32_t N, int64_t C, int64_t size) {
+    return p && p->data ? span_of(p->data, C * size, p->stride * size, N) : Span();
+}
+// A weight gradient may take the place of the weight, row by row: a block has read what it replaces.
+bool may_replace(const liec_param* out, const liec_param* in, int32_t N, int64_t C, int64_t size) {
+    if (in && out && in->data && in->data == out->data && (N == 1 || in->stride == out->stride)) return true;
+    return !spans_meet(span_of_param(out, N, C, size), span_of_param(in, N, C, size));
+}
 LnRows rows_of(const liec_rows* r) { return r ? LnRows{r->data, r->worker_stride, r->row_stride} : LnRows{nullptr, 0, 0}; }
 LnParam param_of(const liec_param* p, int type) { return p && p->data ? LnParam{p->data, p->stride, (uint32_t)type} : LnParam{nullptr, 0, (uint32_t)type}; }
 
@@ -499,7 +507,15 @@ liec_status liec_layer_norm_backward(const liec_rows* dy, const liec_rows* x, co
         if (params && !valid_workspace(workspace, workspace_bytes, liec_layer_norm_workspace(N, R, C))) return LIEC_EINVAL;
     }
     if (params) {
-        if (dweight && dbias && dweight->data && dweight->data == dbias->data) return LIEC_EINVAL;
+        const Span dw = span_of_param(dweight, N, C, psize), db = span_of_param(dbias, N, C, psize);
+        if (spans_meet(dw, db) || !may_replace(dweight, weight, N, C, psize) || !may_replace(dbias, weight, N, C, psize)) return LIEC_EINVAL;
+        if (R)
+            for (const Span& p : {dw, db}) {
+                for (const liec_rows* r : {dy, x, dx})
+                    if (r && spans_meet(p, span_of_rows(r, N, R, C, size))) return LIEC_EINVAL;
+                for (const float* f : {mean, rstd})
+                    if (spans_meet(p, span_of(f, N * R * 4))) return LIEC_EINVAL;
+            }
         // one sum for all workers, or one for each: the same for both gradients
         if (dweight && dweight->data && dbias && dbias->data && N > 1 && (dweight->stride == 0) != (dbias->stride == 0)) return LIEC_EINVAL;
         if (N > 1)

@@ -101,3 +101,26 @@ def test_rows_that_are_written_and_rows_that_are_read(lib):  # noqa: F811
     assert one.forward(x=Rows(MB, 0, S), y=Rows(MB, 0, S + 1)) == EINVAL
     row = _LayerNorm(lib, N, 1, C)
     assert row.backward(dy=Rows(MB, S, 0), dx=Rows(MB, S, 5)) != EINVAL
+
+
+def test_weight_gradients(lib):  # noqa: F811
+    N, R, C, S = 3, 10, 64, 200
+    f = _LayerNorm(lib, N, R, C)
+    at = Param(13 * MB, S)
+    for column, meet in ((0, True), (63, True), (64, False), (136, False), (137, True), (199, True), (200, True), (N * S, False), (-64, False), (-63, True)):
+        assert (f.backward(dw=at, db=Param(13 * MB + 4 * column, S)) == EINVAL) == meet, column
+        assert (f.backward(dw=Param(13 * MB + 4 * column, S), db=at) == EINVAL) == meet, column
+        assert (f.backward(dw=Param(13 * MB + 4 * column, S), w=at) == EINVAL) == (meet and column != 0), column     # w itself may be replaced
+        assert (f.backward(db=Param(13 * MB + 4 * column, S), w=at) == EINVAL) == (meet and column != 0), column
+    assert f.backward(dw=Param(9 * MB + 4 * 64, -S), db=Param(9 * MB, S)) != EINVAL
+    assert f.backward(dw=Param(9 * MB, C), w=Param(9 * MB, 0)) == EINVAL                     # a shared weight in one worker's gradient
+    assert f.backward(dw=Param(9 * MB, 0), db=Param(9 * MB + 4 * 63, 0)) == EINVAL
+    assert f.backward(dw=Param(9 * MB, 0), db=Param(9 * MB + 4 * 64, 0)) != EINVAL
+    for place in ("dy", "x", "dx", "mean", "rstd"):
+        k = {"dy": 1, "x": 2, "dx": 3, "mean": 7, "rstd": 8}[place]
+        size = 4 * N * R * (C if k < 4 else 1)
+        for start, meet in ((k * MB, True), (k * MB + size - 4, True), (k * MB + size, False), (k * MB - 4 * C, False), (k * MB - 4 * C + 4, True)):
+            assert (f.backward(dw=Param(start, 0), db=Param(10 * MB, 0)) == EINVAL) == meet, (place, start)
+            assert (f.backward(db=Param(start, 0), dw=Param(10 * MB, 0)) == EINVAL) == meet, (place, start)
+    empty = _LayerNorm(lib, N, 0, C)
+    assert empty.backward(dw=at, db=Param(13 * MB + 4 * 63, S)) == EINVAL
