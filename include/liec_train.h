@@ -99,13 +99,13 @@ typedef struct {
 /*
  * liec_layer_norm: for every row, mu = mean(x), rstd = 1 / sqrt(mean((x - mu)^2) + eps) and
  * y = (x - mu) * rstd * weight + bias.
- *   mean, rstd   DEVICE fp32 [N, R] contiguous, for the backward pass; either may be NULL
+ *   mean, rstd   DEVICE fp32 [N, R] contiguous, for the backward pass; either may be NULL; memory of their own
  *   dtype        type of x and y;  param_dtype  type of weight and bias
  *   1 <= N <= 65535, 0 <= R < 2^31 (no rows: nothing to do), 1 <= C <= 2^28, at most 2^40 values, eps >= 0 and
  *                finite; no value lies further than 2^40 values from the first
  * y may be x itself (same pointer and strides); otherwise they must not overlap, and neither may y's rows one
  * another (LIEC_EINVAL; at strides that differ, more than 2^22 rows of both that lie between one another count as
- * overlapping).  Rows of 8 to 16384 columns are read once.
+ * overlapping).  y may not share memory with weight or bias.  Rows of 8 to 16384 columns are read once.
  */
 liec_status liec_layer_norm(const liec_rows *x, const liec_param *weight, const liec_param *bias, const liec_rows *y,
                             float *mean, float *rstd, int32_t N, int64_t R, int64_t C, float eps, liec_dtype dtype,
@@ -122,7 +122,7 @@ int64_t liec_layer_norm_workspace(int32_t N, int64_t R, int64_t C);
  * there are no rows (zeros).  They share no memory with each other or with other operands; either may take the place
  * of weight itself (same pointer and stride).
  *   dx           NULL, or data = NULL, where it is not asked for; dx may be dy or x itself (same pointer and strides),
- *                as for liec_layer_norm; its rows must not overlap
+ *                as for liec_layer_norm; its rows must not overlap, nor share memory with mean, rstd or weight
  *   mean, rstd   as liec_layer_norm left them
  *   param_dtype  type of weight, dweight and dbias
  */

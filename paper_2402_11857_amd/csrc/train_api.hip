@@ -479,7 +479,12 @@ liec_status liec_layer_norm(const liec_rows* x, const liec_param* weight, const 
     if (R == 0) return LIEC_OK;
     const int64_t size = size_of(dtype), psize = size_of(param_dtype);
     if (!valid_rows(x, N, R, size) || !valid_rows(y, N, R, size) || !valid_param(weight, psize) || !valid_param(bias, psize)) return LIEC_EINVAL;
-    if (!aligned_to(mean, 4) || !aligned_to(rstd, 4) || (mean && mean == rstd) || !apart(y, N, R, C) || !may_write(y, x, N, R, C, size)) return LIEC_EINVAL;
+    if (!aligned_to(mean, 4) || !aligned_to(rstd, 4) || !apart(y, N, R, C) || !may_write(y, x, N, R, C, size)) return LIEC_EINVAL;
+    const Span ys = span_of_rows(y, N, R, C, size), ws = span_of_param(weight, N, C, psize), bs = span_of_param(bias, N, C, psize);
+    const Span ms = span_of(mean, N * R * 4), rs = span_of(rstd, N * R * 4);
+    if (spans_meet(ms, rs) || spans_meet(ys, ws) || spans_meet(ys, bs)) return LIEC_EINVAL;
+    for (const Span& p : {span_of_rows(x, N, R, C, size), ys, ws, bs})
+        if (spans_meet(ms, p) || spans_meet(rs, p)) return LIEC_EINVAL;
     const LnForward a{rows_of(x), rows_of(y), param_of(weight, param_dtype), param_of(bias, param_dtype), mean, rstd, eps, N, R, C, (hipStream_t)hip_stream};
     if (dtype == LIEC_F32) forward_of<float>(a);
     else if (dtype == LIEC_BF16) forward_of<bf16>(a);
@@ -504,7 +509,16 @@ liec_status liec_layer_norm_backward(const liec_rows* dy, const liec_rows* x, co
         if (!valid_rows(dy, N, R, size) || !valid_rows(x, N, R, size) || (dx && !valid_rows(dx, N, R, size))) return LIEC_EINVAL;
         if (!mean || !rstd || !aligned_to(mean, 4) || !aligned_to(rstd, 4)) return LIEC_EINVAL;
         if (dx && !(apart(dx, N, R, C) && may_write(dx, dy, N, R, C, size) && may_write(dx, x, N, R, C, size))) return LIEC_EINVAL;
-        if (params && !valid_workspace(workspace, workspace_bytes, liec_layer_norm_workspace(N, R, C))) return LIEC_EINVAL;
+        const int64_t need = params ? liec_layer_norm_workspace(N, R, C) : 0;
+        if (params && !valid_workspace(workspace, workspace_bytes, need)) return LIEC_EINVAL;
+        const Span ms = span_of(mean, N * R * 4), rs = span_of(rstd, N * R * 4), ws = span_of_param(weight, N, C, psize), scratch = span_of(workspace, need);
+        if (dx)
+            for (const Span& p : {ms, rs, ws})
+                if (spans_meet(span_of_rows(dx, N, R, C, size), p)) return LIEC_EINVAL;
+        for (const liec_rows* r : {dy, x, dx})
+            if (r && spans_meet(span_of_rows(r, N, R, C, size), scratch)) return LIEC_EINVAL;
+        for (const Span& p : {ms, rs, ws, span_of_param(dweight, N, C, psize), span_of_param(dbias, N, C, psize)})
+            if (spans_meet(p, scratch)) return LIEC_EINVAL;
     }
     if (params) {
         const Span dw = span_of_param(dweight, N, C, psize), db = span_of_param(dbias, N, C, psize);

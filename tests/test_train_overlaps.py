@@ -124,3 +124,34 @@ def test_weight_gradients(lib):  # noqa: F811
             assert (f.backward(db=Param(start, 0), dw=Param(10 * MB, 0)) == EINVAL) == meet, (place, start)
     empty = _LayerNorm(lib, N, 0, C)
     assert empty.backward(dw=at, db=Param(13 * MB + 4 * 63, S)) == EINVAL
+
+
+def test_statistics_weights_and_scratch(lib):  # noqa: F811
+    N, R, C = 3, 10, 64
+    f = _LayerNorm(lib, N, R, C)
+    stat, act, par = 4 * N * R, 4 * N * R * C, 4 * N * C
+
+    def places(start, size, own):
+        """Starts of an operand of `own` bytes around one of `size` bytes, and whether they meet."""
+        return ((start, True), (start + size - 4, True), (start + size, False), (start - own + 4, True), (start - own, False))
+
+    for k, size in ((1, act), (2, act), (5, par), (6, par)):                                 # x, y, weight, bias
+        for start, meet in places(k * MB, size, stat):
+            assert (f.forward(mean=start) == EINVAL) == meet
+            assert (f.forward(rstd=start) == EINVAL) == meet
+    for start, meet in places(7 * MB, stat, stat):
+        assert (f.forward(rstd=start) == EINVAL) == meet
+    assert f.forward(mean=None, rstd=None) != EINVAL
+    for start, meet in places(2 * MB, act, par):
+        assert (f.forward(w=Param(start, C)) == EINVAL) == meet
+        assert (f.forward(b=Param(start, C)) == EINVAL) == meet
+    for start, meet in places(3 * MB, act, stat):
+        assert (f.backward(mean=start) == EINVAL) == meet
+        assert (f.backward(rstd=start) == EINVAL) == meet
+    for start, meet in places(3 * MB, act, par):
+        assert (f.backward(w=Param(start, C)) == EINVAL) == meet
+    assert f.backward(mean=7 * MB, rstd=7 * MB) != EINVAL                                    # only read
+    for k, size in ((1, act), (2, act), (3, act), (5, par), (7, stat), (8, stat), (9, par), (10, par)):
+        start = k * MB + size & -16                          # scratch begins at multiples of 16
+        for ws, meet in ((k * MB, True), (start - 16, True), (start + 16, False), (k * MB - f.need + 16, True), (k * MB - (f.need + 15 & -16), False)):
+            assert (f.backward(ws=ws) == EINVAL) == meet, (k, ws - k * MB)
