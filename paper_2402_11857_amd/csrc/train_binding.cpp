@@ -66,6 +66,11 @@ at::Tensor new_tensor(at::IntArrayRef sizes, at::ScalarType type, const at::Tens
     return at::empty(sizes, at::TensorOptions().dtype(type).device(like.device()));
 }
 
+// A call has written to t: automatic differentiation refuses to use what it saved of it.
+void written(const at::Tensor* t) {
+    if (t && t->defined() && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 void* stream_of(const at::Tensor& t) {
     PyObject* const index = PyLong_FromLong(t.get_device());
     PyObject* const s = index ? PyObject_CallOneArg(g_stream, index) : nullptr;
@@ -96,7 +101,7 @@ void call(const char* name, const at::Tensor& on, F f) {
 
 // ---- gradients -------------------------------------------------------------------------------------------------------
 struct Grads {
-    PyObject* sequence = nullptr;      // held while its tensors are used
+    PyObject* sequence = nullptr;      // a tuple of the tensors, held while they are used
     std::vector<liec_grad_tensor> table;
     int64_t total = 0;
     int32_t N = 0;
@@ -104,16 +109,21 @@ struct Grads {
     at::Tensor workspace;
     int64_t bytes = 0;
     ~Grads() { Py_XDECREF(sequence); }
+    void written_all() const {
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(sequence); ++i) written(&THPVariable_Unpack(PyTuple_GET_ITEM(sequence, i)));
+    }
 };
 
 void read_grads(Grads& g, PyObject* list, const at::Tensor* norms, bool whole) {
     if (THPVariable_Check(list)) type_error("gradients must be a sequence of tensors, not a tensor");
-    g.sequence = PySequence_Fast(list, "gradients must be a sequence of tensors");
+    PyObject* const fast = PySequence_Fast(list, "gradients must be a sequence of tensors");
+    g.sequence = fast ? PySequence_Tuple(fast) : nullptr;
+    Py_XDECREF(fast);
     if (!g.sequence) throw Raise{nullptr, ""};
-    const Py_ssize_t T = PySequence_Fast_GET_SIZE(g.sequence);
+    const Py_ssize_t T = PyTuple_GET_SIZE(g.sequence);
     if (T > LIEC_GRAD_MAX_TENSORS) value_error(std::to_string(T) + " tensors are more than the library takes");
     if (!T && !norms) value_error("no gradients, and no norms to tell the number of workers");
-    g.first = T ? &tensor(PySequence_Fast_GET_ITEM(g.sequence, 0), "a gradient") : norms;
+    g.first = T ? &tensor(PyTuple_GET_ITEM(g.sequence, 0), "a gradient") : norms;
     const c10::Device device = g.first->device();
     if (!g.first->is_cuda()) type_error("gradients must be on the GPU");
     if (norms) {
@@ -126,7 +136,7 @@ void read_grads(Grads& g, PyObject* list, const at::Tensor* norms, bool whole) {
     g.N = (int32_t)N;
     g.table.reserve((size_t)T);
     for (Py_ssize_t i = 0; i < T; ++i) {
-        const at::Tensor& t = tensor(PySequence_Fast_GET_ITEM(g.sequence, i), "a gradient");
+        const at::Tensor& t = tensor(PyTuple_GET_ITEM(g.sequence, i), "a gradient");
         const int code = code_of(t);
         if (code < 0 || t.device() != device) type_error("gradients must be float32, bfloat16 or float16 tensors on one GPU");
         int64_t count = t.numel(), stride = count;
@@ -163,6 +173,7 @@ PyObject* grad_norm(PyObject* const* a) {      // grads, norms, whole
     call("liec_grad_norm", *g.first,
          [&] { return p_grad_norm(g.table.data(), (int32_t)g.table.size(), g.N, data_of(norms), g.workspace.data_ptr(), g.bytes, st); });
     if (made.defined()) return THPVariable_Wrap(made);
+    written(norms);
     Py_INCREF(a[1]);
     return a[1];
 }
@@ -175,6 +186,8 @@ PyObject* clip_grads(PyObject* const* a) {     // grads, max_norm, norms, whole
     void* const st = stream_of(*g.first);
     call("liec_clip_grads", *g.first,
          [&] { return p_clip_grads(g.table.data(), (int32_t)g.table.size(), g.N, bound, data_of(norms), g.workspace.data_ptr(), g.bytes, st); });
+    g.written_all();
+    written(norms);
     Py_RETURN_NONE;
 }
 
@@ -193,6 +206,8 @@ PyObject* gather_grads(PyObject* const* a) {   // grads, rows, max_norm, norms, 
         return p_gather_grads(g.table.data(), (int32_t)g.table.size(), g.N, static_cast<float*>(rows.data_ptr()), rows.stride(0), bound, data_of(norms),
                               g.workspace.data_ptr(), g.bytes, st);
     });
+    written(&rows);
+    written(norms);
     Py_RETURN_NONE;
 }
 
@@ -314,6 +329,7 @@ PyObject* layer_norm(PyObject* const* a) {     // x, weight, bias, eps, out
     call("liec_layer_norm", x, [&] {
         return p_layer_norm(&xr, &w, &b, &yr, data_of(&mean), data_of(&rstd), N, s.R, s.C, (float)eps, (liec_dtype)code, (liec_dtype)pcode, st);
     });
+    written(out);
     if (out) Py_INCREF(a[4]);
     PyObject* const first = out ? a[4] : THPVariable_Wrap(y);
     PyObject* const second = first ? THPVariable_Wrap(mean) : nullptr;
@@ -357,6 +373,7 @@ PyObject* layer_norm_backward(PyObject* const* a) {   // dy, x, mean, rstd, weig
         return p_layer_norm_backward(&gr, &xr, data_of(&mean), data_of(&rstd), &w, &dr, &dw, &db, N, s.R, s.C, (liec_dtype)code, (liec_dtype)pcode,
                                      bytes ? ws.data_ptr() : nullptr, bytes, st);
     });
+    for (const at::Tensor* t : {given, dweight, dbias}) written(t);
     if (!need) Py_RETURN_NONE;
     if (!given) return THPVariable_Wrap(dx);
     Py_INCREF(a[5]);

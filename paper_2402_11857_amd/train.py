@@ -4,6 +4,10 @@ Tensors of N workers carry the workers as their leading dimension.  Every functi
 stream of the tensors' device and returns; scratch comes from torch's allocator.  Arguments are checked and marshalled by
 the compiled module ``_train.so``: TypeError for types and devices, ValueError for shapes and strides, LiecError for what
 the library refuses.  There is no CPU fallback.
+
+The functions are not differentiable: results carry no history, whether or not the operands require a gradient, so call
+liec_layer_norm_backward for one.  Tensors that a function writes to count as changed in place, so automatic
+differentiation notices where it had saved their values.
 """
 from __future__ import annotations
 
