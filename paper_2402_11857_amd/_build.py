@@ -49,17 +49,26 @@ def build_library(verbose: bool = False, defines=(), out: str = LIB_PATH) -> str
 BINDING_PATH = os.path.join(_HERE, "_train.so")
 
 
+def host_compiler() -> str:
+    """A C++ compiler for host code: the system's, or the one that comes with hipcc."""
+    for cand in (shutil.which("g++"), shutil.which("c++"), os.path.join(os.path.dirname(hipcc()), "amdclang++")):
+        if cand and os.path.exists(cand):
+            return cand
+    raise RuntimeError("no C++ compiler found: the binding cannot be built")
+
+
 def build_binding(verbose: bool = False) -> str:
-    """Always recompiles the Python side of include/liec_train.h (host code only, against torch's headers)."""
+    """Always recompiles the Python side of include/liec_train.h (host code only, against the headers of Python and torch).  The
+    compressed step does not need it."""
     import sysconfig
 
     from torch.utils import cpp_extension
 
-    cxx = shutil.which("g++") or shutil.which("c++")
-    if not cxx:
-        raise RuntimeError("g++ not found: the binding cannot be built")
-    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-I", os.path.join(_ROOT, "include")]
-    for path in cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]:
+    python = sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(python, "Python.h")):
+        raise RuntimeError(f"{os.path.join(python, 'Python.h')} not found: the binding cannot be built without Python's headers")
+    cmd = [host_compiler(), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-I", os.path.join(_ROOT, "include")]
+    for path in cpp_extension.include_paths() + [python]:
         cmd += ["-isystem", path]
     cmd += [os.path.join(_HERE, "csrc", "train_binding.cpp"), "-o", BINDING_PATH]
     for path in cpp_extension.library_paths():
