@@ -13,8 +13,8 @@
  * every failure is a status code of liec.h (LIEC_EINVAL: nothing was enqueued).
  *
  * Arithmetic: inputs are widened to fp32 exactly, results are rounded once to the output's type, to nearest; sums of
- * squares of gradients are carried in fp64, the sums of layer normalisation in fp32 or more.  The order of every sum is fixed
- * by the sizes, so equal calls give equal bits.
+ * squares of gradients are carried in fp64, the sums of layer normalisation in fp32 over at most 256 rows or one row's
+ * columns and in fp64 beyond.  The order of every sum is fixed by the sizes, so equal calls give equal bits.
  */
 #ifndef LIEC_TRAIN_H
 #define LIEC_TRAIN_H
@@ -51,8 +51,8 @@ int64_t liec_grads_workspace(int32_t N, int32_t T);
  * liec_grad_norm: norms[i] = sqrt(sum over the T tensors of the squares of worker i's values), i < N (DEVICE, fp32,
  * N values).  Infinities and NaN show in the norm of their worker, and only there.  T = 0 or no values: zero.
  *   1 <= N <= 65535, 0 <= T <= LIEC_GRAD_MAX_TENSORS, at most 2^35 values per worker.  stride may be anything, 0
- *   included (workers that share a tensor).  Two kernels; one more for every 184 further
- *   tensors (128 where a tensor's stride is not its count).
+ *   included (workers that share a tensor).  Two kernels; one more for every 184 further tensors (128 where a tensor's
+ *   stride is not its count).
  */
 liec_status liec_grad_norm(const liec_grad_tensor *tensors, int32_t T, int32_t N, float *norms, void *workspace,
                            int64_t workspace_bytes, void *hip_stream);
@@ -78,7 +78,8 @@ liec_status liec_clip_grads(const liec_grad_tensor *tensors, int32_t T, int32_t 
  * so are norms in the rows.  At strides that
  * differ from the rows', more than 2^22 workers' values that lie between the rows count as sharing.
  *   row_stride  >= the sum of the counts
- *   max_norm = +Inf with norms = NULL only gathers: one kernel for up to 128 tensors, each value read once.
+ *   max_norm = +Inf with norms = NULL only gathers: one kernel for up to 184 tensors (128 where a tensor's stride is not
+ *   its count), each value read once.
  */
 liec_status liec_gather_grads(const liec_grad_tensor *tensors, int32_t T, int32_t N, float *rows, int64_t row_stride,
                               float max_norm, float *norms, void *workspace, int64_t workspace_bytes, void *hip_stream);

@@ -5,9 +5,9 @@
 // The tensors of all workers are cut into tiles of kGradTile consecutive bytes of one tensor and one worker; a tile is read
 // by one wave, with 16-byte accesses whatever its alignment (a tile per block of four waves left three of them idle on small
 // tensors: 161 tensors of 52 x 158 043 fp16 values 36 us, now 12).  Both kernels are bound by memory, and both sweep it in the
-// order of their blocks: squares are added up by waves that stay on the chip, take every B-th tile of one worker and have the
-// next one's loads under way (consecutive tiles: 5 % slower), scaling is done by a wave per tile.  Measured: 32 x 25.6M bf16
-// values squared at 6.7 TB/s, 16 x 11.7M fp32 values squared and scaled in 353 us, 6.4 TB/s over both passes.
+// order of their blocks: squares are added up by at most 4096 blocks, whose waves take every B-th tile of one worker and have
+// the next one's loads under way (consecutive tiles: 5 % slower), scaling is done by a wave per tile.  Measured: 32 x 25.6M bf16
+// values squared at 6.7 TB/s, 16 x 11.7M fp32 values squared and scaled in 355 us, 6.4 TB/s over both passes.
 #pragma once
 #include "elements.hpp"
 
@@ -63,7 +63,7 @@ struct Tile {
     int64_t col;                       // column of its first element
 };
 
-// The tensor that holds tile `tile`: the last one that starts at or before it.  Every lane looks at three starts.
+// The tensor that holds tile `tile`: the last one that starts at or before it.  Every lane looks at two starts, or three.
 template <bool STRIDED>
 __device__ __forceinline__ uint32_t tensor_of(const GradTable<STRIDED>& tab, uint32_t count, uint32_t tile) {
     const uint32_t lane = lane_id();

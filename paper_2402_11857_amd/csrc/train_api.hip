@@ -19,15 +19,16 @@ namespace {
 
 constexpr int32_t kMaxWorkers = 65535;
 constexpr int64_t kMaxGradValues = (int64_t)1 << 35;
-// Thread blocks of a launch that adds up squares, 16 per compute unit, twice what is resident at a time (norm of 16 x 11.7M
+// Thread blocks of a launch that adds up squares, 16 per compute unit; six of them are resident at a time (norm of 16 x 11.7M
 // fp32 values: 2048 blocks 123 us, 4096 114).
 constexpr int64_t kGradBlocks = 4096;
-// Partial sums of a worker that the blocks of the scaling kernel add up again, each of them (138M values of one worker
-// clipped: 512 blocks 283 us, 1024 263, 2048 273, 4096 295).
+// Blocks of a launch whose partial sums the blocks of the scaling kernel add up again, each of them (138M values of one worker
+// clipped: 512 blocks 283 us, 1024 263, 2048 273, 4096 295).  Several launches leave up to 4096 partial sums in all.
 constexpr int64_t kGradParts = 1024;
-// Gradients of one worker that exceed the memory-side cache are squared and scaled before the next worker's, so that part of
-// them is still there (16 x 138M bf16 values into rows 2814 against 3168 us); shorter ones leave the chip idle between so many
-// launches (8 x 50M 788 against 598 us).
+// Workers with more gradients than this are squared and scaled one after the other, all others together: many launches against a
+// second pass that finds nothing of the first in the caches.  One by one and together, 16 workers in bf16: clipped, 100 MB each 905
+// against 783 to 806 us, 220 MB 1790 against 1748 to 1798, 270 MB 2180 against 2169 to 2230, 330 MB 2648 against 2664 to 2738; into
+// rows 100 MB 1049 against 1122 to 1141, 270 MB 2746 against 3169 to 3241.  Rows would gain from 140 MB on (4 workers: 352 against 364).
 constexpr int64_t kGradRowBytes = (int64_t)256 << 20;
 
 bool valid_type(int t) { return t == LIEC_F32 || t == LIEC_BF16 || t == LIEC_F16; }
