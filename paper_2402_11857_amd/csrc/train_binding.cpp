@@ -259,7 +259,7 @@ Sizes sizes_of(const at::Tensor& x, std::initializer_list<const at::Tensor*> par
     N = 1;
     for (int64_t split = 0; rows && split < std::max<int64_t>(1, dims - 1); N *= x.size(split++)) {
         const Sizes s{N, rows / N, C, split};
-        bool all = N <= 65535;
+        bool all = N <= 65535 && s.R < ((int64_t)1 << 31);       // what the library takes
         liec_rows r;
         for (const at::Tensor* t : operands) all = all && (!t || as_rows(*t, s, &r));
         if (all) return s;

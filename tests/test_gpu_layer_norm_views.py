@@ -92,3 +92,13 @@ def test_rows_in_two_groups_of_dimensions():
     view.copy_(x)
     _forward_and_backward(view, dy, w, b)
     _forward_and_backward(x, dy, w, b, out=view.clone(memory_format=torch.preserve_format), dx=view)
+
+
+def test_more_rows_than_one_worker_may_have():
+    import paper_2402_11857_amd as pkg
+
+    say("case layer norm, 2^31 rows of an expanded tensor, arguments only")
+    shape = (2, 1 << 30, 8)                                  # nothing is asked for, so nothing is computed
+    x = torch.ones(8, dtype=torch.bfloat16, device=DEV).expand(shape)
+    mean = torch.empty(shape[:2], device=DEV)
+    assert pkg.liec_layer_norm_backward(x, x, mean, mean, need_dx=False) is None
