@@ -39,3 +39,11 @@ from .train import (  # noqa: F401
     liec_layer_norm,
     liec_layer_norm_backward,
 )
+from .activations import (  # noqa: F401
+    Checkpoint,
+    liec_checkpoint_load,
+    liec_checkpoint_save,
+    liec_group_norm,
+    liec_group_norm_backward,
+    liec_weight_grad,
+)

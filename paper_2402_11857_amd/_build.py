@@ -1,19 +1,21 @@
 """Compiles the HIP library for gfx950 in-tree (paper_2402_11857_amd/libliec.so)."""
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import shutil
 import subprocess
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_HERE)
 LIB_PATH = os.path.join(_HERE, "libliec.so")
-SOURCES = [os.path.join(_HERE, "csrc", n) for n in ("liec_api.hip", "train_api.hip")]
-HEADERS = [os.path.join(_HERE, "csrc", "liec_kernels.hpp"), os.path.join(_HERE, "csrc", "spans.hpp"), os.path.join(_ROOT, "include", "liec.h"),
-           os.path.join(_ROOT, "include", "liec_testing.h"), os.path.join(_ROOT, "include", "liec_train.h")] + \
+SOURCES = [os.path.join(_HERE, "csrc", n) for n in ("liec_api.hip", "train_api.hip", "activations_api.hip")]
+HEADERS = [os.path.join(_HERE, "csrc", n) for n in ("liec_kernels.hpp", "operands.hpp", "spans.hpp")] + \
+          [os.path.join(_ROOT, "include", n) for n in ("liec.h", "liec_testing.h", "liec_train.h", "liec_activations.h")] + \
           [os.path.join(_HERE, "csrc", "kernels", n)
-           for n in ("common.hpp", "elements.hpp", "grads.hpp", "layer_norm.hpp", "rows.hpp", "select.hpp", "sign.hpp", "step.hpp", "sync.hpp",
-                     "telemetry.hpp", "wire.hpp")]
+           for n in ("checkpoint.hpp", "common.hpp", "elements.hpp", "grads.hpp", "group_norm.hpp", "layer_norm.hpp", "rows.hpp", "select.hpp", "sign.hpp",
+                     "step.hpp", "sync.hpp", "telemetry.hpp", "weight_grad.hpp", "wire.hpp")]
 
 
 def hipcc() -> str:
@@ -29,20 +31,26 @@ def build_library(verbose: bool = False, defines=(), out: str = LIB_PATH) -> str
     the first struct passed by value on, are in scalar registers when a wave starts instead of being loaded by every wave (short
     kernels gain most: 8 scaled-sign messages of 11.7M + 1 columns 101.7 -> 98.9 us, averaging 27 x 109160 13.6 -> 13.0, top-k
     8 x 1M 53.2 -> 52.2; long ones are even).  `defines` (NAME=value strings) and `out`
-    let a tuning run build a variant of the library beside the product's."""
-    cmd = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
-           "-ffp-contract=off", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-           "-mllvm", "-amdgpu-kernarg-preload-count=16",
-           "-Wall", "-Wno-unused-command-line-argument"] + [f"-D{d}" for d in defines] + [
-           "-I", os.path.join(_ROOT, "include"), "-I", os.path.join(_HERE, "csrc"),
-           "-o", out] + SOURCES
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
-    if verbose and res.stderr.strip():
-        print(res.stderr)
+    let a tuning run build a variant of the library beside the product's.  The sources are compiled side by side."""
+    flags = [hipcc(), "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+             "-ffp-contract=off", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
+             "-mllvm", "-amdgpu-kernarg-preload-count=16",
+             "-Wall", "-Wno-unused-command-line-argument"] + [f"-D{d}" for d in defines] + [
+             "-I", os.path.join(_ROOT, "include"), "-I", os.path.join(_HERE, "csrc")]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        res = subprocess.run(cmd, capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
+        if verbose and res.stderr.strip():
+            print(res.stderr)
+
+    with tempfile.TemporaryDirectory() as tmp, concurrent.futures.ThreadPoolExecutor(len(SOURCES)) as pool:
+        objects = [os.path.join(tmp, os.path.basename(src) + ".o") for src in SOURCES]
+        list(pool.map(lambda pair: run(flags + ["-c", pair[0], "-o", pair[1]]), zip(SOURCES, objects)))
+        run([hipcc(), "--offload-arch=gfx950", "-fPIC", "-shared", "-o", out] + objects)
     return out
 
 
@@ -58,8 +66,8 @@ def host_compiler() -> str:
 
 
 def build_binding(verbose: bool = False) -> str:
-    """Always recompiles the Python side of include/liec_train.h (host code only, against the headers of Python and torch).  The
-    compressed step does not need it."""
+    """Always recompiles the Python side of include/liec_train.h and include/liec_activations.h (host code only, against the headers
+    of Python and torch).  The compressed step does not need it."""
     import sysconfig
 
     from torch.utils import cpp_extension
@@ -70,7 +78,7 @@ def build_binding(verbose: bool = False) -> str:
     cmd = [host_compiler(), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall", "-I", os.path.join(_ROOT, "include")]
     for path in cpp_extension.include_paths() + [python]:
         cmd += ["-isystem", path]
-    cmd += [os.path.join(_HERE, "csrc", "train_binding.cpp"), "-o", BINDING_PATH]
+    cmd += [os.path.join(_HERE, "csrc", n) for n in ("train_binding.cpp", "activations_binding.cpp")] + ["-o", BINDING_PATH]
     for path in cpp_extension.library_paths():
         cmd += ["-L", path]
     cmd += ["-lc10", "-ltorch_cpu", "-ltorch_python"]

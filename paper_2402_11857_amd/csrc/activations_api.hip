@@ -1,0 +1,410 @@
+// Host side of include/liec_activations.h: argument checks, launch shapes, launches.
+#include "liec_activations.h"
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "kernels/group_norm.hpp"
+#include "kernels/weight_grad.hpp"
+#include "operands.hpp"
+
+using namespace liec;
+
+namespace {
+
+// Results of up to the memory-side cache's 256 MB are left there for the operation that reads them next.
+bool keeps(int64_t bytes) { return bytes <= (int64_t)256 << 20; }
+
+// Blocks of a launch whose blocks walk over the work: far more than are resident, and within what a launch may have.
+uint32_t grid_of(int64_t works) { return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(works, (int64_t)1 << 22)); }
+
+LnRows rows_of(const liec_rows* r) { return LnRows{r->data, r->worker_stride, r->row_stride}; }
+LnParam param_of(const liec_param* p, int type) { return p && p->data ? LnParam{p->data, p->stride, (uint32_t)type} : LnParam{nullptr, 0, (uint32_t)type}; }
+
+// ---- checkpoints -----------------------------------------------------------------------------------------------------
+constexpr int64_t kMostRows = ((int64_t)1 << 31) - 1;
+
+bool valid_sizes(int64_t N, int64_t R, int64_t C) {
+    if ((double)N * (double)R * (double)C > (double)kMostValues) return false;
+    return N >= 1 && N <= kMaxWorkers && R >= 0 && R <= kMostRows && C >= 1 && C <= ((int64_t)1 << 28);
+}
+bool valid_saved(const liec_checkpoint* s) { return s && s->values && s->exponents; }
+Saved saved_of(const liec_checkpoint* s) { return s ? Saved{s->values, s->exponents} : Saved{nullptr, nullptr}; }
+int64_t groups_of(int64_t C) { return ceil_div(C, kSavedCols); }
+Span span_of_values(const liec_checkpoint* s, int64_t rows, int64_t C) { return s ? span_of(s->values, rows * C) : Span(); }
+Span span_of_exponents(const liec_checkpoint* s, int64_t rows, int64_t C) { return s ? span_of(s->exponents, rows * groups_of(C)) : Span(); }
+
+struct SavedLaunch {
+    dim3 grid;
+    uint32_t per, magic;
+};
+SavedLaunch saved_launch(int64_t N, int64_t R, int64_t C) {
+    const int64_t per = 4 * groups_of(C);
+    return {dim3(grid_of(ceil_div(R * per, kSavedBlock)), (uint32_t)N), (uint32_t)per, (uint32_t)((((uint64_t)1 << 32) + per - 1) / per)};
+}
+// Workers whose rows follow one another are one worker's: a short one fills no block.
+void merge_workers(LnRows& r, int64_t& N, int64_t& R) {
+    if (N > 1 && r.worker == R * r.row && N * R <= kMostRows) R *= N, N = 1;
+}
+
+template <typename T>
+void run_save(LnRows x, const Saved& to, int64_t N, int64_t R, int64_t C, hipStream_t st) {
+    merge_workers(x, N, R);
+    const SavedLaunch l = saved_launch(N, R, C);
+    k_checkpoint_save<T><<<l.grid, kBlock, 0, st>>>(R, (uint32_t)C, l.per, l.magic, x, to);
+}
+template <typename T>
+void run_load(const Saved& from, LnRows y, int64_t N, int64_t R, int64_t C, hipStream_t st) {
+    const bool keep = keeps(N * R * C * (int64_t)sizeof(T));
+    merge_workers(y, N, R);
+    const SavedLaunch l = saved_launch(N, R, C);
+    k_checkpoint_load<T><<<l.grid, kBlock, 0, st>>>(R, (uint32_t)C, l.per, l.magic, keep, from, y);
+}
+
+// ---- group normalisation ---------------------------------------------------------------------------------------------
+// Images as an operand: the runs of each worker's images, or of all of them where workers follow one another.
+struct ImageSpans {
+    int64_t first, wide, many;         // bytes between groups of runs
+    int64_t len, s, n, t, m;           // a group: m times at distances t, n runs of len at distances s
+    Span at(int64_t i) const { return span_of((const void*)(first + i * wide), len, s, n, t, m); }
+};
+ImageSpans image_spans(const liec_images* x, int64_t N, int64_t B, int64_t S, int64_t C, int64_t size) {
+    const int64_t w = x->worker_stride * size, b = x->image_stride * size, r = x->row_stride * size, at = (int64_t)(uintptr_t)x->data;
+    if (N == 1 || w == B * b) return {at, 0, 1, C * size, r, S, b, N * B};
+    if (B == 1 || b == S * r) return {at, 0, 1, C * size, r, B * S, w, N};
+    return {at, w, N, C * size, r, S, b, B};
+}
+bool images_meet(const ImageSpans& a, const Span& p) {
+    int64_t steps = kSpanSteps;
+    for (int64_t i = 0; i < a.many; ++i)
+        if (--steps < 0 || spans_meet(a.at(i), p, steps)) return true;
+    return false;
+}
+bool images_meet(const ImageSpans& a, const ImageSpans& b) {
+    int64_t steps = kSpanSteps;
+    for (int64_t i = 0; i < a.many; ++i)
+        for (int64_t j = 0; j < b.many; ++j)
+            if (--steps < 0 || spans_meet(a.at(i), b.at(j), steps)) return true;
+    return false;
+}
+// Rows that are written must not share memory: each distance spans what the narrower ones cover.
+bool apart(const liec_images* x, int64_t N, int64_t B, int64_t S, int64_t C) {
+    std::pair<int64_t, int64_t> d[3] = {{llabs(x->row_stride), S}, {llabs(x->image_stride), B}, {llabs(x->worker_stride), N}};
+    std::sort(d, d + 3);
+    int64_t covered = C;
+    for (const auto& [stride, n] : d) {
+        if (n == 1) continue;
+        if (stride < covered) return false;
+        covered += (n - 1) * stride;
+    }
+    return true;
+}
+bool same(const liec_images* a, const liec_images* b, int64_t N, int64_t B, int64_t S) {
+    return a->data == b->data && (N == 1 || a->worker_stride == b->worker_stride) && (B == 1 || a->image_stride == b->image_stride) &&
+           (S == 1 || a->row_stride == b->row_stride);
+}
+bool valid_images(const liec_images* x, int64_t N, int64_t B, int64_t S, int64_t size) {
+    if (!x || !x->data || !aligned_to(x->data, size) || !in_range(x->worker_stride) || !in_range(x->image_stride) || !in_range(x->row_stride)) return false;
+    return (double)(S - 1) * (double)llabs(x->row_stride) + (double)(B - 1) * (double)llabs(x->image_stride) + (double)(N - 1) * (double)llabs(x->worker_stride) <=
+           (double)kMostValues;
+}
+
+bool valid_norm(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
+    if (N < 1 || N > kMaxWorkers || B < 0 || B > kMostRows || S < 0 || S > kMostRows || C < 1 || C > ((int64_t)1 << 20)) return false;
+    if (G < 1 || G > C || C % G) return false;
+    return (double)N * (double)B * (double)std::max<int64_t>(S, 1) * (double)C <= (double)kMostValues;
+}
+
+constexpr int64_t kGnBlocks = 4096;    // that a launch should have at least, where there is work for them
+constexpr int64_t kGnChain = 256;      // positions that a thread adds up
+
+int log_of(int64_t n) {                // of the next power of two
+    int r = 0;
+    while (((int64_t)1 << r) < n) ++r;
+    return r;
+}
+
+GnShape shape_of(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
+    GnShape s{};
+    const int64_t pieces = C < 8 ? C : ceil_div(C, 8);
+    s.images = N * B, s.B = B, s.S = S, s.C = (uint32_t)C, s.G = (uint32_t)G, s.per_group = (uint32_t)(C / G);
+    // four lanes at least where a row is not shorter: those that share an exponent of a checkpoint
+    s.lanes_log = (uint32_t)std::min(6, C < 8 ? log_of(C) : std::max(2, log_of(pieces)));
+    s.tiles = (uint32_t)ceil_div(pieces, (int64_t)1 << s.lanes_log);
+    const int64_t threads = kBlock >> s.lanes_log;
+    const int64_t want = ceil_div(kGnBlocks, std::max<int64_t>(1, s.images * s.tiles));
+    s.per = std::max(ceil_div(S, want), std::min(S, kGnAhead * threads));
+    s.per = std::max<int64_t>(1, std::min(s.per, kGnChain * threads));
+    s.splits = (uint32_t)std::max<int64_t>(1, ceil_div(S, s.per));
+    return s;
+}
+int64_t gn_works_of(const GnShape& s) { return s.images * s.splits * s.tiles; }
+uint32_t gn_group_blocks(const GnShape& s) { return grid_of(ceil_div(s.images * s.G, kBlock / 64)); }
+int64_t gn_partials(const GnShape& s) { return s.images * s.splits * 2 * (int64_t)s.C; }
+GnImages images_of(const liec_images* x) { return x && x->data ? GnImages{x->data, x->worker_stride, x->image_stride, x->row_stride} : GnImages{nullptr, 0, 0, 0}; }
+
+struct GnForward {
+    GnShape s;
+    GnImages x, y;
+    LnParam w, b;
+    float *mean, *rstd, *partial, eps;
+    Saved saved;
+    bool keep;
+    int act;
+    hipStream_t st;
+};
+
+template <typename T, int V>
+void gn_forward_of(const GnForward& a) {
+    const uint32_t grid = grid_of(gn_works_of(a.s));
+    k_gn_stats<T, V><<<grid, kBlock, 0, a.st>>>(a.s, a.x, a.partial);
+    k_gn_groups<0><<<gn_group_blocks(a.s), kBlock, 0, a.st>>>(a.s, a.partial, a.eps, a.mean, a.rstd);
+    const auto apply = a.act == kActNone ? k_gn_apply<T, V, kActNone> : a.act == kActRelu ? k_gn_apply<T, V, kActRelu> : k_gn_apply<T, V, kActSilu>;
+    apply<<<grid, kBlock, 0, a.st>>>(a.s, a.keep, a.mean, a.rstd, a.x, a.y, a.w, a.b, a.saved);
+}
+template <typename T>
+void gn_forward_of(const GnForward& a) { a.s.C < 8 ? gn_forward_of<T, 1>(a) : gn_forward_of<T, 8>(a); }
+
+struct GnBackward {
+    GnShape s;
+    GnImages dy, x, dx;
+    Saved saved;
+    LnParam w, b, dw, db;
+    const float *mean, *rstd;
+    float* partial;
+    bool keep;
+    hipStream_t st;
+};
+
+template <typename T, int V, int ACT, bool SAVED>
+void gn_backward_of(const GnBackward& a) {
+    const uint32_t grid = grid_of(gn_works_of(a.s));
+    k_gn_sums<T, V, ACT, SAVED><<<grid, kBlock, 0, a.st>>>(a.s, a.mean, a.rstd, a.dy, a.x, a.saved, a.w, a.b, a.partial);
+    if (!a.dx.data) return;
+    float2* const means = reinterpret_cast<float2*>(a.partial + gn_partials(a.s));
+    k_gn_means<0><<<gn_group_blocks(a.s), kBlock, 0, a.st>>>(a.s, a.partial, a.w, means);
+    k_gn_dx<T, V, ACT, SAVED><<<grid, kBlock, 0, a.st>>>(a.s, a.keep, a.mean, a.rstd, means, a.dy, a.x, a.saved, a.dx, a.w, a.b);
+}
+template <typename T, int V, int ACT>
+void gn_backward_of(const GnBackward& a) { a.saved.q ? gn_backward_of<T, V, ACT, true>(a) : gn_backward_of<T, V, ACT, false>(a); }
+template <typename T, int V>
+void gn_backward_of(const GnBackward& a, int act) {
+    act == kActNone ? gn_backward_of<T, V, kActNone>(a) : act == kActRelu ? gn_backward_of<T, V, kActRelu>(a) : gn_backward_of<T, V, kActSilu>(a);
+}
+template <typename T>
+void gn_backward_of(const GnBackward& a, int act) { a.s.C < 8 ? gn_backward_of<T, 1>(a, act) : gn_backward_of<T, 8>(a, act); }
+
+bool valid_act(int a) { return a == LIEC_ACT_NONE || a == LIEC_ACT_RELU || a == LIEC_ACT_SILU; }
+
+// ---- weight gradients ------------------------------------------------------------------------------------------------
+constexpr int64_t kWgChain = 8192;     // rows that are added up in fp32
+constexpr int64_t kWgStep = 64;        // rows that a split is a multiple of
+constexpr int64_t kWgBlocks = 512;     // that a launch should have at least, where there are rows for them
+
+bool valid_weight(int64_t N, int64_t R, int64_t O, int64_t C) {
+    if (N < 1 || N > kMaxWorkers || R < 0 || R > kMostRows || O < 1 || C < 1 || O > ((int64_t)1 << 24) || C > ((int64_t)1 << 24)) return false;
+    const double n = (double)N, most = (double)kMostValues;
+    return n * (double)O * (double)C <= most && n * (double)R * (double)O <= most && n * (double)R * (double)C <= most;
+}
+
+int64_t wg_tile(int64_t O, int64_t C) { return O > 64 && C > 64 ? 128 : 64; }
+
+WgShape weight_shape(int64_t N, int64_t R, int64_t O, int64_t C) {
+    WgShape s{};
+    const int64_t tile = wg_tile(O, C);
+    s.N = (uint32_t)N, s.R = R, s.O = O, s.C = C;
+    s.tiles_o = (uint32_t)ceil_div(O, tile), s.tiles_c = (uint32_t)ceil_div(C, tile);
+    const int64_t blocks = N * s.tiles_o * (int64_t)s.tiles_c;
+    int64_t splits = std::max<int64_t>(1, std::min(kWgBlocks / blocks, R / (4 * kWgStep)));
+    splits = std::max(splits, ceil_div(R, kWgChain));
+    s.per = std::max(kWgStep, ceil_div(ceil_div(R, splits), kWgStep) * kWgStep);
+    s.splits = (uint32_t)std::max<int64_t>(1, ceil_div(R, s.per));
+    return s;
+}
+
+template <typename T>
+void weight_grad_of(const WgShape& s, const LnRows& dy, const Saved& x, const WgOut& dw, const LnParam& db, float* partial, hipStream_t st) {
+    const uint32_t grid = grid_of((int64_t)s.N * s.splits * s.tiles_o * s.tiles_c);
+    constexpr int BK = sizeof(T) == 4 ? 32 : 64;
+    if (wg_tile(s.O, s.C) == 128) k_weight_grad<T, 128, 128, BK, 2, 2><<<grid, 256, 0, st>>>(s, dy, x, dw, db, partial);
+    else k_weight_grad<T, 64, 64, 64, 2, 2><<<grid, 256, 0, st>>>(s, dy, x, dw, db, partial);
+    if (partial) k_weight_grad_join<0><<<dim3(grid_of(ceil_div(s.O * (s.C + 1), kBlock)), s.N), kBlock, 0, st>>>(s, partial, dw, db);
+}
+
+}  // namespace
+
+extern "C" {
+
+liec_status liec_checkpoint_save(const liec_rows* x, const liec_checkpoint* saved, int32_t N, int64_t R, int64_t C, liec_dtype dtype, void* hip_stream) {
+    if (!valid_sizes(N, R, C) || !valid_type(dtype)) return LIEC_EINVAL;
+    if (R == 0) return LIEC_OK;
+    const int64_t size = size_of(dtype), rows = N * R;
+    if (!valid_rows(x, N, R, size) || !valid_saved(saved)) return LIEC_EINVAL;
+    const Span xs = span_of_rows(x, N, R, C, size), qs = span_of_values(saved, rows, C), es = span_of_exponents(saved, rows, C);
+    if (spans_meet(xs, qs) || spans_meet(xs, es) || spans_meet(qs, es)) return LIEC_EINVAL;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const LnRows from = rows_of(x);
+    const Saved to = saved_of(saved);
+    if (dtype == LIEC_F32) run_save<float>(from, to, N, R, C, st);
+    else if (dtype == LIEC_BF16) run_save<bf16>(from, to, N, R, C, st);
+    else run_save<f16>(from, to, N, R, C, st);
+    return launched();
+}
+
+liec_status liec_checkpoint_load(const liec_checkpoint* saved, const liec_rows* y, int32_t N, int64_t R, int64_t C, liec_dtype dtype, void* hip_stream) {
+    if (!valid_sizes(N, R, C) || !valid_type(dtype)) return LIEC_EINVAL;
+    if (R == 0) return LIEC_OK;
+    const int64_t size = size_of(dtype), rows = N * R;
+    if (!valid_rows(y, N, R, size) || !valid_saved(saved) || !apart(y, N, R, C)) return LIEC_EINVAL;
+    const Span ys = span_of_rows(y, N, R, C, size);
+    if (spans_meet(ys, span_of_values(saved, rows, C)) || spans_meet(ys, span_of_exponents(saved, rows, C))) return LIEC_EINVAL;
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const LnRows to = rows_of(y);
+    const Saved from = saved_of(saved);
+    if (dtype == LIEC_F32) run_load<float>(from, to, N, R, C, st);
+    else if (dtype == LIEC_BF16) run_load<bf16>(from, to, N, R, C, st);
+    else run_load<f16>(from, to, N, R, C, st);
+    return launched();
+}
+
+int64_t liec_group_norm_workspace(int32_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
+    if (!valid_norm(N, B, S, C, G)) return -1;
+    if (B == 0 || S == 0) return 0;
+    const GnShape s = shape_of(N, B, S, C, G);
+    return gn_partials(s) * (int64_t)sizeof(float) + s.images * G * (int64_t)sizeof(float2);
+}
+
+liec_status liec_group_norm(const liec_images* x, const liec_param* weight, const liec_param* bias, const liec_images* y, float* mean, float* rstd,
+                            const liec_checkpoint* saved, int32_t N, int64_t B, int64_t S, int64_t C, int64_t G, float eps, liec_activation activation,
+                            liec_dtype dtype, liec_dtype param_dtype, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    if (!valid_norm(N, B, S, C, G) || !valid_type(dtype) || !valid_type(param_dtype) || !valid_act(activation) || !(eps >= 0.f) || !isfinite(eps)) return LIEC_EINVAL;
+    if (B == 0 || S == 0) return LIEC_OK;
+    const int64_t size = size_of(dtype), psize = size_of(param_dtype), need = liec_group_norm_workspace(N, B, S, C, G), stats = (int64_t)N * B * G * 4;
+    if (!valid_images(x, N, B, S, size) || !valid_images(y, N, B, S, size) || !valid_param(weight, psize) || !valid_param(bias, psize)) return LIEC_EINVAL;
+    if (!mean || !rstd || !aligned_to(mean, 4) || !aligned_to(rstd, 4) || (saved && !valid_saved(saved))) return LIEC_EINVAL;
+    if (!valid_workspace(workspace, workspace_bytes, need) || !apart(y, N, B, S, C)) return LIEC_EINVAL;
+    const ImageSpans xs = image_spans(x, N, B, S, C, size), ys = image_spans(y, N, B, S, C, size);
+    if (!same(x, y, N, B, S) && images_meet(xs, ys)) return LIEC_EINVAL;
+    // what is written, apart from y, and what is read, apart from x
+    const Span written[] = {span_of(mean, stats), span_of(rstd, stats), span_of_values(saved, N * B * S, C), span_of_exponents(saved, N * B * S, C), span_of(workspace, need)};
+    const Span read[] = {span_of_param(weight, N, C, psize), span_of_param(bias, N, C, psize)};
+    for (const Span& r : read)
+        if (images_meet(ys, r)) return LIEC_EINVAL;
+    for (const Span& w : written) {
+        if (images_meet(xs, w) || images_meet(ys, w)) return LIEC_EINVAL;
+        for (const Span& r : read)
+            if (spans_meet(w, r)) return LIEC_EINVAL;
+        for (const Span& v : written)
+            if (&v < &w && spans_meet(v, w)) return LIEC_EINVAL;
+    }
+    const GnForward a{shape_of(N, B, S, C, G), images_of(x), images_of(y), param_of(weight, param_dtype), param_of(bias, param_dtype), mean, rstd,
+                      static_cast<float*>(workspace), eps, saved_of(saved), keeps((int64_t)N * B * S * C * size), activation, (hipStream_t)hip_stream};
+    if (dtype == LIEC_F32) gn_forward_of<float>(a);
+    else if (dtype == LIEC_BF16) gn_forward_of<bf16>(a);
+    else gn_forward_of<f16>(a);
+    return launched();
+}
+
+liec_status liec_group_norm_backward(const liec_images* dy, const liec_images* x, const liec_checkpoint* saved, const float* mean, const float* rstd,
+                                     const liec_param* weight, const liec_param* bias, const liec_images* dx, const liec_param* dweight,
+                                     const liec_param* dbias, int32_t N, int64_t B, int64_t S, int64_t C, int64_t G, liec_activation activation,
+                                     liec_dtype dtype, liec_dtype param_dtype, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    if (!valid_norm(N, B, S, C, G) || !valid_type(dtype) || !valid_type(param_dtype) || !valid_act(activation)) return LIEC_EINVAL;
+    const int64_t size = size_of(dtype), psize = size_of(param_dtype), need = liec_group_norm_workspace(N, B, S, C, G), stats = (int64_t)N * B * G * 4;
+    if (x && !x->data) x = nullptr;
+    if (saved && !saved->values) saved = nullptr;
+    if (dx && !dx->data) dx = nullptr;
+    if (dweight && !dweight->data) dweight = nullptr;
+    if (dbias && !dbias->data) dbias = nullptr;
+    for (const liec_param* p : {weight, bias, dweight, dbias})
+        if (!valid_param(p, psize)) return LIEC_EINVAL;
+    if (N > 1) {
+        for (const liec_param* p : {dweight, dbias})
+            if (p && p->stride && llabs(p->stride) < C) return LIEC_EINVAL;
+        // one sum for all workers, or one for each: the same for both gradients
+        if (dweight && dbias && (dweight->stride == 0) != (dbias->stride == 0)) return LIEC_EINVAL;
+    }
+    const Span dws = span_of_param(dweight, N, C, psize), dbs = span_of_param(dbias, N, C, psize), ws = span_of_param(weight, N, C, psize),
+               bs = span_of_param(bias, N, C, psize);
+    if (spans_meet(dws, dbs)) return LIEC_EINVAL;
+    for (const Span& r : {ws, bs})
+        if (spans_meet(dws, r) || spans_meet(dbs, r)) return LIEC_EINVAL;
+    const bool empty = B == 0 || S == 0;
+    if (!empty) {
+        if (!valid_images(dy, N, B, S, size) || (x && !valid_images(x, N, B, S, size)) || (dx && !valid_images(dx, N, B, S, size))) return LIEC_EINVAL;
+        if (!x == !saved || (saved && !valid_saved(saved))) return LIEC_EINVAL;
+        if (!mean || !rstd || !aligned_to(mean, 4) || !aligned_to(rstd, 4) || !valid_workspace(workspace, workspace_bytes, need)) return LIEC_EINVAL;
+        const Span read[] = {span_of(mean, stats), span_of(rstd, stats), span_of_values(saved, N * B * S, C), span_of_exponents(saved, N * B * S, C), ws, bs};
+        const Span written[] = {dws, dbs, span_of(workspace, need)};
+        for (const Span& w : written) {
+            for (const liec_images* m : {dy, x, dx})
+                if (m && images_meet(image_spans(m, N, B, S, C, size), w)) return LIEC_EINVAL;
+            for (const Span& r : read)
+                if (spans_meet(w, r)) return LIEC_EINVAL;
+        }
+        if (spans_meet(written[2], dws) || spans_meet(written[2], dbs)) return LIEC_EINVAL;
+        if (dx) {
+            const ImageSpans out = image_spans(dx, N, B, S, C, size);
+            if (!apart(dx, N, B, S, C)) return LIEC_EINVAL;
+            for (const liec_images* m : {dy, x})
+                if (m && !same(dx, m, N, B, S) && images_meet(out, image_spans(m, N, B, S, C, size))) return LIEC_EINVAL;
+            for (const Span& r : read)
+                if (images_meet(out, r)) return LIEC_EINVAL;
+        }
+    }
+    const hipStream_t st = (hipStream_t)hip_stream;
+    GnBackward a{shape_of(N, B, S, C, G), images_of(dy), images_of(x), images_of(dx), saved_of(saved), param_of(weight, param_dtype), param_of(bias, param_dtype),
+                 param_of(dweight, param_dtype), param_of(dbias, param_dtype), mean, rstd, static_cast<float*>(workspace),
+                 keeps((int64_t)N * B * S * C * size), st};
+    if (!empty && (dx || dweight || dbias)) {
+        if (dtype == LIEC_F32) gn_backward_of<float>(a, activation);
+        else if (dtype == LIEC_BF16) gn_backward_of<bf16>(a, activation);
+        else gn_backward_of<f16>(a, activation);
+    }
+    if (dweight || dbias) {
+        const bool shared = N == 1 || (dweight ? dweight : dbias)->stride == 0;
+        const int64_t parts = empty ? 0 : (shared ? a.s.images : B) * (int64_t)a.s.splits;
+        k_gn_param_grads<0><<<dim3((uint32_t)ceil_div(C, 32), shared ? 1u : (uint32_t)N, 2), kBlock, 0, st>>>(a.partial, parts, (uint32_t)C, a.dw, a.db);
+    }
+    return launched();
+}
+
+int64_t liec_weight_grad_workspace(int32_t N, int64_t R, int64_t O, int64_t C) {
+    if (!valid_weight(N, R, O, C)) return -1;
+    const WgShape s = weight_shape(N, R, O, C);
+    return s.splits > 1 ? s.splits * (int64_t)N * O * (C + 1) * (int64_t)sizeof(float) : 0;
+}
+
+liec_status liec_weight_grad(const liec_rows* dy, const liec_checkpoint* saved, const liec_matrices* dweight, const liec_param* dbias, int32_t N, int64_t R, int64_t O,
+                             int64_t C, liec_dtype dtype, liec_dtype param_dtype, void* workspace, int64_t workspace_bytes, void* hip_stream) {
+    if (!valid_weight(N, R, O, C) || !valid_type(dtype) || !valid_type(param_dtype)) return LIEC_EINVAL;
+    const int64_t size = size_of(dtype), psize = size_of(param_dtype), need = liec_weight_grad_workspace(N, R, O, C);
+    if (dbias && !dbias->data) dbias = nullptr;
+    if (!dweight) return LIEC_EINVAL;
+    const liec_rows out{dweight->data, dweight->worker_stride, dweight->row_stride};
+    if (!valid_rows(&out, N, O, psize) || !apart(&out, N, O, C) || !valid_param(dbias, psize)) return LIEC_EINVAL;
+    if (dbias && N > 1 && llabs(dbias->stride) < O) return LIEC_EINVAL;
+    if (need && !valid_workspace(workspace, workspace_bytes, need)) return LIEC_EINVAL;
+    const Span dws = span_of_rows(&out, N, O, C, psize), dbs = span_of_param(dbias, N, O, psize), scratch = span_of(workspace, need);
+    if (spans_meet(dws, dbs) || spans_meet(dws, scratch) || spans_meet(dbs, scratch)) return LIEC_EINVAL;
+    if (R) {
+        if (!valid_rows(dy, N, R, size) || !valid_saved(saved)) return LIEC_EINVAL;
+        for (const Span& r : {span_of_rows(dy, N, R, O, size), span_of_values(saved, N * R, C), span_of_exponents(saved, N * R, C)})
+            if (spans_meet(dws, r) || spans_meet(dbs, r) || spans_meet(scratch, r)) return LIEC_EINVAL;
+    }
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const WgShape s = weight_shape(N, R, O, C);
+    const LnRows g = R ? rows_of(dy) : LnRows{nullptr, 0, 0};
+    const WgOut dw{dweight->data, dweight->worker_stride, dweight->row_stride, (uint32_t)param_dtype};
+    const LnParam db = param_of(dbias, param_dtype);
+    const Saved from = R ? saved_of(saved) : Saved{nullptr, nullptr};
+    float* const partial = s.splits > 1 ? static_cast<float*>(workspace) : nullptr;
+    if (dtype == LIEC_F32) weight_grad_of<float>(s, g, from, dw, db, partial, st);
+    else if (dtype == LIEC_BF16) weight_grad_of<bf16>(s, g, from, dw, db, partial, st);
+    else weight_grad_of<f16>(s, g, from, dw, db, partial, st);
+    return launched();
+}
+
+}  // extern "C"

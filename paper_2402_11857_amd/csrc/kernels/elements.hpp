@@ -131,6 +131,16 @@ __device__ __forceinline__ void st16_as(bool keep, T* p, v4u v) {
     }
 }
 
+struct LnRows {                        // a [workers, rows, columns] tensor of unit column stride
+    void* data;
+    int64_t worker, row;               // strides, in elements
+};
+struct LnParam {                       // a [workers, columns] tensor of unit column stride; stride 0: one row for all workers
+    void* data;
+    int64_t stride;
+    uint32_t type;
+};
+
 // 4 values of 16 bits as one streaming load.
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t v2u_any2 __attribute__((ext_vector_type(2), aligned(2)));

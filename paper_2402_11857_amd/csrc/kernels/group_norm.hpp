@@ -1,0 +1,533 @@
+// Group normalisation with an activation function, channels last, of N workers' images, each worker with weights of its own, and
+// its gradients.
+//
+//   forward    mu, var over the S positions and the C / G channels of a group,  rstd = 1 / sqrt(var + eps),
+//              y = act((x - mu) rstd w + b)
+//   backward   h = (x - mu) rstd,  z = h w + b,  dz = dy act'(z),  a = dz w,  dx = rstd (a - mean a - h mean(a h))
+//              dw = sum over the worker's images and positions of dz h,  db of dz
+//
+// Everything starts from sums per image and channel: with P1_c = sum_s dz and P2_c = sum_s dz h, mean a and mean(a h) are sums of
+// w_c P1_c and w_c P2_c over a group's channels, dw and db those of P2_c and P1_c over images; forward, a channel's mean and squares
+// around it go together in the group's.  So a thread keeps 8 channels and walks positions, whatever the groups' width, and loads are
+// 16 bytes wide.  The last 8 channels of a row whose length is no multiple of 8 start 8 before its end; what they share with
+// the ones before is left out where it is stored.
+#pragma once
+#include "checkpoint.hpp"
+
+namespace liec {
+
+enum Act : int { kActNone = 0, kActRelu = 1, kActSilu = 2 };
+
+struct GnImages {                      // an [N, B, S, C] tensor of unit channel stride
+    void* data;
+    int64_t worker, image, row;        // strides, in elements
+};
+
+struct GnShape {
+    int64_t images, B, S;              // images = N * B
+    uint32_t C, G, per_group;
+    uint32_t lanes_log;                // a row-thread's lanes, each with 8 channels (one, where C < 8): tiles of the channels
+    uint32_t tiles, splits;            // a block's work: one tile, `per` of an image's positions
+    int64_t per;
+};
+
+// ---- activation ------------------------------------------------------------------------------------------------------
+// exp(-z) with the product's rounding error put right, to about 2 u; at most 2^126, so that its reciprocal is a number.
+__device__ __forceinline__ float exp_minus(float z) {
+    const float log2e = 1.44269502f, rest = 1.92596299e-8f;              // their sum is log2(e)
+    const float t = -z * log2e, off = __fmaf_rn(-z, rest, __fmaf_rn(-z, log2e, -t));
+    const float e = __builtin_amdgcn_exp2f(fminf(t, 126.f));
+    return fabsf(t) < 126.f ? __fmaf_rn(e, off * 0.693147181f, e) : e;
+}
+
+template <int ACT>
+__device__ __forceinline__ float act_of(float z) {
+    if (ACT == kActRelu) return z < 0.f ? 0.f : z;
+    if (ACT == kActSilu) return z * __builtin_amdgcn_rcpf(1.f + exp_minus(z));
+    return z;
+}
+
+// dz and h of a value.  The sign of z decides a ReLU's gradient: in fp32 z is off by at most 2 u |h w| + u |z|, so it is right unless
+// |z| <= 4 u |b| (then |h w| <= |b| (1 + 4 u)), and such a value is looked at in fp64.
+template <int ACT>
+__device__ __forceinline__ float dz_of(float dy, float x, float mu, float rs, float w, float b, float& h) {
+    h = (x - mu) * rs;
+    if (ACT == kActNone) return dy;
+    const float z = __fmaf_rn(h, w, b);
+    if (ACT == kActRelu) {
+        bool on = z > 0.f;
+        if (__builtin_expect(fabsf(z) <= 0x1p-22f * fabsf(b), 0)) on = ((double)x - (double)mu) * (double)rs * (double)w + (double)b > 0.0;
+        return on ? dy : 0.f;
+    }
+    const float e = exp_minus(z), p = __builtin_amdgcn_rcpf(1.f + e);
+    return dy * (p * __fmaf_rn(z, e * p, 1.f));                          // p (1 + z (1 - p)),  1 - p = e p
+}
+
+// ---- a thread's channels ----------------------------------------------------------------------------------------------
+struct GnColumns {
+    uint32_t c, skip;                  // first channel it loads, how many of them belong to the thread before
+    bool any;
+};
+template <int V>
+__device__ __forceinline__ GnColumns gn_columns(const GnShape& s, uint32_t tile, uint32_t lane) {
+    const uint32_t at = ((tile << s.lanes_log) + lane) * V;
+    GnColumns r;
+    r.any = at < s.C;
+    r.c = V == 1 ? at : min(at, s.C - V);
+    r.skip = at - r.c;
+    return r;
+}
+
+// x as it lies in memory: a tensor's row or a checkpoint's.
+template <typename T, int V, bool SAVED>
+struct GnRaw {
+    Eight<T> v;
+    __device__ __forceinline__ void load(const T* row, const GnColumns& k) { v = ld_eight<T, false>(row + k.c); }
+    __device__ __forceinline__ void widen(const GnColumns&, float (&f)[V]) const { widen_eight<T>(v, f); }
+};
+template <typename T>
+struct GnRaw<T, 1, false> {
+    T v;
+    __device__ __forceinline__ void load(const T* row, const GnColumns& k) { v = row[k.c]; }
+    __device__ __forceinline__ void widen(const GnColumns&, float (&f)[1]) const { f[0] = liec::widen(v); }
+};
+template <typename T>
+struct GnRaw<T, 8, true> {
+    v2u w;
+    uint32_t e;                        // the last channel's exponent, and that of every channel that is not left out
+    __device__ __forceinline__ void load(const Saved& s, int64_t row, uint32_t C, uint32_t groups, const GnColumns& k) {
+        w = ld8_bytes(s.q + row * C + k.c);
+        e = s.e[row * groups + (k.c + 7) / kSavedCols];
+    }
+    __device__ __forceinline__ void widen(const GnColumns&, float (&f)[8]) const {
+        unpack4(w.x, saved_scale(e), f);
+        unpack4(w.y, saved_scale(e), f + 4);
+    }
+};
+template <typename T>
+struct GnRaw<T, 1, true> {
+    int8_t q;
+    uint8_t e;
+    __device__ __forceinline__ void load(const Saved& s, int64_t row, uint32_t C, uint32_t groups, const GnColumns& k) {
+        q = s.q[row * C + k.c];
+        e = s.e[row * groups];
+    }
+    __device__ __forceinline__ void widen(const GnColumns&, float (&f)[1]) const { f[0] = (float)q * saved_scale(e); }
+};
+
+template <typename T>
+__device__ __forceinline__ T* gn_image(const GnImages& m, const GnShape& s, int64_t image) {
+    const int64_t worker = image / s.B;
+    return static_cast<T*>(m.data) + worker * m.worker + (image - worker * s.B) * m.image;
+}
+
+struct GnWork {
+    uint32_t tile, split;
+    int64_t image, first, end;         // positions
+};
+__device__ __forceinline__ GnWork gn_work(const GnShape& s, int64_t work) {
+    GnWork r;
+    const int64_t strip = work / s.tiles;
+    r.tile = (uint32_t)(work - strip * s.tiles);
+    r.image = strip / s.splits;
+    r.split = (uint32_t)(strip - r.image * s.splits);
+    r.first = r.split * s.per;
+    r.end = min(r.first + s.per, s.S);
+    return r;
+}
+__device__ __forceinline__ int64_t gn_works(const GnShape& s) { return s.images * s.splits * s.tiles; }
+
+constexpr int kGnAhead = 4;            // positions of a thread requested together
+constexpr int kGnTile = 512;           // channels of a tile, at most
+
+// Stores a block's sums per channel, lds[wave][channel of the tile] of `waves` waves put together by `join`.
+template <int V, typename F>
+__device__ __forceinline__ void gn_store_channels(const GnShape& s, const GnWork& w, F value, float* out) {
+    for (uint32_t t = threadIdx.x; t < (uint32_t)(V << s.lanes_log); t += kBlock) {
+        const GnColumns k = gn_columns<V>(s, w.tile, t / V);
+        if (k.any && t % V >= k.skip) {
+            const float2 v = value(t);
+            float* const to = out + (size_t)(w.image * s.splits + w.split) * 2 * s.C + k.c + t % V;
+            to[0] = v.x;
+            to[s.C] = v.y;
+        }
+    }
+}
+
+// ---- forward ----------------------------------------------------------------------------------------------------------
+// Mean and squares around it of n and n2 values, put together.
+__device__ __forceinline__ void gn_join(float n, float& mean, float& squares, float n2, float mean2, float squares2) {
+    const float all = n + n2, share = all > 0.f ? n2 / all : 0.f, d = mean2 - mean;
+    mean = __fmaf_rn(d, share, mean);
+    squares += __fmaf_rn(d * d, n * share, squares2);
+}
+
+// Mean and squares around it of each channel over a strip of an image's positions.  A thread takes its values around the mean p of its
+// first four: with n of them (at most 256) and m their mean, (p - m)^2 <= n / 4 of their variance, so that taking n (p - m)^2 off
+// again costs at most 64 u of it per addition's u.
+template <typename T, int V>
+__global__ __launch_bounds__(kBlock) void k_gn_stats(GnShape s, GnImages x, float* __restrict__ partial) {
+    __shared__ float lds_mean[kBlock / 64][kGnTile], lds_squares[kBlock / 64][kGnTile], lds_n[kBlock / 64];
+    const uint32_t lane = threadIdx.x & ((1u << s.lanes_log) - 1), thread = threadIdx.x >> s.lanes_log, threads = kBlock >> s.lanes_log;
+    for (int64_t work = blockIdx.x; work < gn_works(s); work += gridDim.x) {
+        const GnWork w = gn_work(s, work);
+        const GnColumns k = gn_columns<V>(s, w.tile, lane);
+        const T* const at = gn_image<const T>(x, s, w.image);
+        float p[V], sum[V], squares[V], n = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) p[j] = sum[j] = squares[j] = 0.f;
+        for (int64_t r = w.first + thread; k.any && r < w.end; r += kGnAhead * threads) {
+            GnRaw<T, V, false> raw[kGnAhead];
+            const uint32_t rows = (uint32_t)min((int64_t)kGnAhead, (w.end - r + threads - 1) / threads);
+#pragma unroll
+            for (int u = 0; u < kGnAhead; ++u) raw[u].load(at + (u < (int)rows ? r + u * threads : r) * x.row, k);
+            float f[kGnAhead][V];
+#pragma unroll
+            for (int u = 0; u < kGnAhead; ++u) raw[u].widen(k, f[u]);
+            if (n == 0.f) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float t = f[0][j];
+                    for (int u = 1; u < kGnAhead; ++u) t += u < (int)rows ? f[u][j] : 0.f;
+                    p[j] = t / (float)rows;
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kGnAhead; ++u) {
+                if (u >= (int)rows) break;
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float d = f[u][j] - p[j];
+                    sum[j] += d;
+                    squares[j] = __fmaf_rn(d, d, squares[j]);
+                }
+            }
+            n += (float)rows;
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float d = n > 0.f ? sum[j] / n : 0.f;
+            p[j] += d;
+            squares[j] = fmaxf(__fmaf_rn(-d, sum[j], squares[j]), 0.f) + (d - d);      // a NaN stays one
+        }
+        for (uint32_t off = 1u << s.lanes_log; off < 64; off <<= 1) {
+            const float n2 = __shfl_xor(n, off);
+#pragma unroll
+            for (int j = 0; j < V; ++j) gn_join(n, p[j], squares[j], n2, __shfl_xor(p[j], off), __shfl_xor(squares[j], off));
+            n += n2;
+        }
+        const uint32_t wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == lane) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                lds_mean[wave][lane * V + j] = p[j];
+                lds_squares[wave][lane * V + j] = squares[j];
+            }
+            if (lane == 0) lds_n[wave] = n;
+        }
+        __syncthreads();
+        gn_store_channels<V>(s, w, [&](uint32_t t) {
+            float many = lds_n[0];
+            float2 v = make_float2(lds_mean[0][t], lds_squares[0][t]);
+            for (int i = 1; i < kBlock / 64; ++i) {
+                gn_join(many, v.x, v.y, lds_n[i], lds_mean[i][t], lds_squares[i][t]);
+                many += lds_n[i];
+            }
+            return v;
+        }, partial);
+        __syncthreads();
+    }
+}
+
+// A wave goes over what an image's strips left of a group's channels: neighbouring lanes on neighbouring channels.
+template <typename F>
+__device__ __forceinline__ void gn_each_part(const GnShape& s, int64_t group, F f) {
+    const int64_t image = group / s.G;
+    const uint32_t first = (uint32_t)(group - image * s.G) * s.per_group, lane = threadIdx.x & 63;
+    const uint32_t wide_log = s.per_group >= 64 ? 6 : 32 - __clz((int)s.per_group), wide = 1u << wide_log;
+    for (uint32_t split = lane >> wide_log; split < s.splits; split += 64 >> wide_log)
+        for (uint32_t c = lane & (wide - 1); c < s.per_group; c += wide) f((size_t)(image * s.splits + split) * 2 * s.C + first + c, first + c, split);
+}
+
+__device__ __forceinline__ int64_t gn_wave() { return (int64_t)blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6); }
+
+template <int>
+__global__ __launch_bounds__(kBlock) void k_gn_groups(GnShape s, const float* __restrict__ partial, float eps, float* __restrict__ mean, float* __restrict__ rstd) {
+    for (int64_t g = gn_wave(); g < s.images * s.G; g += (int64_t)gridDim.x * (kBlock / 64)) {
+        const int64_t image = g / s.G;
+        const double p = (double)partial[(size_t)image * s.splits * 2 * s.C + (uint32_t)(g - image * s.G) * s.per_group];
+        double sum = 0.0, squares = 0.0;
+        gn_each_part(s, g, [&](size_t at, uint32_t, uint32_t split) {
+            const double n = (double)min(s.per, s.S - split * s.per), d = (double)partial[at] - p;
+            sum += n * d;
+            squares += (double)partial[at + s.C] + n * d * d;
+        });
+        sum = wave_sum(sum);
+        squares = wave_sum(squares);
+        const double n = (double)s.S * (double)s.per_group, d = sum / n, var = (squares - d * sum) / n;
+        if ((threadIdx.x & 63) == 0) {
+            mean[g] = (float)(p + d);
+            rstd[g] = (float)(1.0 / sqrt((var > 0.0 ? var : var - var) + (double)eps));
+        }
+    }
+}
+
+// Bits of the largest magnitude of a checkpoint's group of columns: the lanes that share it.
+template <int V>
+__device__ __forceinline__ uint32_t gn_largest(uint32_t a, uint32_t lanes_log) {
+    if (V == 8) return max_of_quad(a);
+    for (uint32_t off = 1; off < 1u << lanes_log; off <<= 1) a = max(a, (uint32_t)__shfl_xor((int)a, off));
+    return a;
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void gn_store(bool keep, T* row, const GnColumns& k, const float (&f)[V]) {
+    if constexpr (V == 8) {
+        if (k.skip == 0) {
+            st_eight<T>(keep, row + k.c, f);
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        if (j >= (int)k.skip) row[k.c + j] = narrow<T>(f[j]);
+}
+
+// The checkpoint of a thread's channels of a row; all lanes that share an exponent call it together.
+template <int V>
+__device__ __forceinline__ void gn_save(const Saved& out, int64_t row, const GnShape& s, const GnColumns& k, const float (&f)[V]) {
+    uint32_t a = 0;
+#pragma unroll
+    for (int j = 0; j < V; ++j) a = max(a, k.any && j >= (int)k.skip ? key_of(f[j]) : 0u);
+    const uint32_t e = saved_exponent(gn_largest<V>(a, s.lanes_log));
+    if (!k.any) return;
+    int8_t* const to = out.q + row * s.C + k.c;
+    const uint32_t first = k.c + k.skip;
+    if (first % kSavedCols == 0) out.e[row * ((s.C + kSavedCols - 1) / kSavedCols) + first / kSavedCols] = (uint8_t)e;
+    if constexpr (V == 8) {
+        const v2u w = pack8(f, e);
+        if (k.skip == 0) {
+            st8_bytes(to, w);
+        } else {
+#pragma unroll
+            for (int j = 1; j < 8; ++j)
+                if (j >= (int)k.skip) to[j] = (int8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3)));
+        }
+    } else {
+        to[0] = e == kSavedNan ? 0 : (int8_t)(int)rintf((e == (uint32_t)kSavedMost ? saved_in_range(f[0]) : f[0]) * saved_inverse(e));
+    }
+}
+
+template <int V>
+struct GnParams {
+    float mu[V], rs[V], w[V], b[V];
+    __device__ __forceinline__ void load(const GnShape& s, int64_t image, const GnColumns& k, const float* mean, const float* rstd, const LnParam& weight,
+                                         const LnParam& bias) {
+        const int64_t worker = image / s.B;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const uint32_t c = k.any ? k.c + j : 0u;
+            const int64_t g = image * s.G + c / s.per_group;
+            mu[j] = mean[g];
+            rs[j] = rstd[g];
+            w[j] = weight.data ? load_any(weight.data, worker * weight.stride + c, weight.type) : 1.f;
+            b[j] = bias.data ? load_any(bias.data, worker * bias.stride + c, bias.type) : 0.f;
+        }
+    }
+};
+
+// y, and the checkpoint of x where `out.q` is there.
+template <typename T, int V, int ACT>
+__global__ __launch_bounds__(kBlock) void k_gn_apply(GnShape s, bool keep, const float* __restrict__ mean, const float* __restrict__ rstd, GnImages x, GnImages y,
+                                                     LnParam weight, LnParam bias, Saved out) {
+    const uint32_t lane = threadIdx.x & ((1u << s.lanes_log) - 1), thread = threadIdx.x >> s.lanes_log, threads = kBlock >> s.lanes_log;
+    for (int64_t work = blockIdx.x; work < gn_works(s); work += gridDim.x) {
+        const GnWork w = gn_work(s, work);
+        const GnColumns k = gn_columns<V>(s, w.tile, lane);
+        const T* const from = gn_image<const T>(x, s, w.image);
+        T* const to = gn_image<T>(y, s, w.image);
+        GnParams<V> p;
+        p.load(s, w.image, k, mean, rstd, weight, bias);
+#pragma unroll
+        for (int j = 0; j < V; ++j) p.rs[j] *= p.w[j];
+        for (int64_t r = w.first + thread; r < w.end; r += kGnAhead * threads) {
+            GnRaw<T, V, false> raw[kGnAhead];
+            const int rows = (int)min((int64_t)kGnAhead, (w.end - r + threads - 1) / threads);
+            if (k.any) {
+#pragma unroll
+                for (int u = 0; u < kGnAhead; ++u) raw[u].load(from + (u < rows ? r + u * threads : r) * x.row, k);
+            }
+#pragma unroll
+            for (int u = 0; u < kGnAhead; ++u) {
+                if (u >= rows) break;
+                float f[V];
+                if (k.any) raw[u].widen(k, f);
+                if (out.q) gn_save<V>(out, w.image * s.S + r + u * threads, s, k, f);
+                if (!k.any) continue;
+#pragma unroll
+                for (int j = 0; j < V; ++j) f[j] = act_of<ACT>(__fmaf_rn(f[j] - p.mu[j], p.rs[j], p.b[j]));
+                gn_store<T, V>(keep, to + (r + u * threads) * y.row, k, f);
+            }
+        }
+    }
+}
+
+// ---- backward ---------------------------------------------------------------------------------------------------------
+template <typename T, int V, bool SAVED>
+__device__ __forceinline__ void gn_load(GnRaw<T, V, SAVED>& raw, const T* image, const GnImages& x, const Saved& saved, const GnShape& s, const GnWork& w, int64_t r,
+                                        const GnColumns& k) {
+    if constexpr (SAVED) raw.load(saved, w.image * s.S + r, s.C, (s.C + kSavedCols - 1) / kSavedCols, k);
+    else raw.load(image + r * x.row, k);
+}
+
+// Sums of dz h and of dz over a strip of an image's positions.
+template <typename T, int V, int ACT, bool SAVED>
+__global__ __launch_bounds__(kBlock) void k_gn_sums(GnShape s, const float* __restrict__ mean, const float* __restrict__ rstd, GnImages dy, GnImages x, Saved saved,
+                                                    LnParam weight, LnParam bias, float* __restrict__ partial) {
+    __shared__ float lds_h[kBlock / 64][kGnTile], lds_1[kBlock / 64][kGnTile];
+    const uint32_t lane = threadIdx.x & ((1u << s.lanes_log) - 1), thread = threadIdx.x >> s.lanes_log, threads = kBlock >> s.lanes_log;
+    for (int64_t work = blockIdx.x; work < gn_works(s); work += gridDim.x) {
+        const GnWork w = gn_work(s, work);
+        const GnColumns k = gn_columns<V>(s, w.tile, lane);
+        const T* const xs = SAVED ? nullptr : gn_image<const T>(x, s, w.image);
+        const T* const gs = gn_image<const T>(dy, s, w.image);
+        GnParams<V> p;
+        p.load(s, w.image, k, mean, rstd, weight, bias);
+        float sum_h[V], sum_1[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum_h[j] = sum_1[j] = 0.f;
+        for (int64_t r = w.first + thread; k.any && r < w.end; r += kGnAhead * threads) {
+            GnRaw<T, V, SAVED> raw[kGnAhead];
+            GnRaw<T, V, false> grad[kGnAhead];
+            const int rows = (int)min((int64_t)kGnAhead, (w.end - r + threads - 1) / threads);
+#pragma unroll
+            for (int u = 0; u < kGnAhead; ++u) {
+                const int64_t at = u < rows ? r + u * threads : r;
+                gn_load<T, V, SAVED>(raw[u], xs, x, saved, s, w, at, k);
+                grad[u].load(gs + at * dy.row, k);
+            }
+#pragma unroll
+            for (int u = 0; u < kGnAhead; ++u) {
+                if (u >= rows) break;
+                float f[V], g[V], h;
+                raw[u].widen(k, f);
+                grad[u].widen(k, g);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float dz = dz_of<ACT>(g[j], f[j], p.mu[j], p.rs[j], p.w[j], p.b[j], h);
+                    sum_1[j] += dz;
+                    sum_h[j] = __fmaf_rn(dz, h, sum_h[j]);
+                }
+            }
+        }
+        for (uint32_t off = 1u << s.lanes_log; off < 64; off <<= 1) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                sum_h[j] += __shfl_xor(sum_h[j], off);
+                sum_1[j] += __shfl_xor(sum_1[j], off);
+            }
+        }
+        const uint32_t wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == lane) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                lds_h[wave][lane * V + j] = sum_h[j];
+                lds_1[wave][lane * V + j] = sum_1[j];
+            }
+        }
+        __syncthreads();
+        gn_store_channels<V>(s, w, [&](uint32_t t) {
+            float2 v = make_float2(lds_h[0][t], lds_1[0][t]);
+            for (int i = 1; i < kBlock / 64; ++i) {
+                v.x += lds_h[i][t];
+                v.y += lds_1[i][t];
+            }
+            return v;
+        }, partial);
+        __syncthreads();
+    }
+}
+
+// Means of a and of a h over a group: pairs [images, G].
+template <int>
+__global__ __launch_bounds__(kBlock) void k_gn_means(GnShape s, const float* __restrict__ partial, LnParam weight, float2* __restrict__ means) {
+    for (int64_t g = gn_wave(); g < s.images * s.G; g += (int64_t)gridDim.x * (kBlock / 64)) {
+        const int64_t worker = g / s.G / s.B;
+        double sum_h = 0.0, sum_1 = 0.0;
+        gn_each_part(s, g, [&](size_t at, uint32_t c, uint32_t) {
+            const double w = weight.data ? (double)load_any(weight.data, worker * weight.stride + c, weight.type) : 1.0;
+            sum_h += w * (double)partial[at];
+            sum_1 += w * (double)partial[at + s.C];
+        });
+        sum_h = wave_sum(sum_h);
+        sum_1 = wave_sum(sum_1);
+        const double n = (double)s.S * (double)s.per_group;
+        if ((threadIdx.x & 63) == 0) means[g] = make_float2((float)(sum_1 / n), (float)(sum_h / n));
+    }
+}
+
+template <typename T, int V, int ACT, bool SAVED>
+__global__ __launch_bounds__(kBlock) void k_gn_dx(GnShape s, bool keep, const float* __restrict__ mean, const float* __restrict__ rstd, const float2* __restrict__ means,
+                                                  GnImages dy, GnImages x, Saved saved, GnImages dx, LnParam weight, LnParam bias) {
+    const uint32_t lane = threadIdx.x & ((1u << s.lanes_log) - 1), thread = threadIdx.x >> s.lanes_log, threads = kBlock >> s.lanes_log;
+    for (int64_t work = blockIdx.x; work < gn_works(s); work += gridDim.x) {
+        const GnWork w = gn_work(s, work);
+        const GnColumns k = gn_columns<V>(s, w.tile, lane);
+        if (!k.any) continue;
+        const T* const xs = SAVED ? nullptr : gn_image<const T>(x, s, w.image);
+        const T* const gs = gn_image<const T>(dy, s, w.image);
+        T* const to = gn_image<T>(dx, s, w.image);
+        GnParams<V> p;
+        p.load(s, w.image, k, mean, rstd, weight, bias);
+        float2 m[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) m[j] = means[w.image * s.G + (k.c + j) / s.per_group];
+        for (int64_t r = w.first + thread; r < w.end; r += kGnAhead * threads) {
+            GnRaw<T, V, SAVED> raw[kGnAhead];
+            GnRaw<T, V, false> grad[kGnAhead];
+            const int rows = (int)min((int64_t)kGnAhead, (w.end - r + threads - 1) / threads);
+#pragma unroll
+            for (int u = 0; u < kGnAhead; ++u) {
+                const int64_t at = u < rows ? r + u * threads : r;
+                gn_load<T, V, SAVED>(raw[u], xs, x, saved, s, w, at, k);
+                grad[u].load(gs + at * dy.row, k);
+            }
+#pragma unroll
+            for (int u = 0; u < kGnAhead; ++u) {
+                if (u >= rows) break;
+                float f[V], g[V], h;
+                raw[u].widen(k, f);
+                grad[u].widen(k, g);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const float dz = dz_of<ACT>(g[j], f[j], p.mu[j], p.rs[j], p.w[j], p.b[j], h);
+                    f[j] = p.rs[j] * (__fmaf_rn(dz, p.w[j], -m[j].x) - h * m[j].y);
+                }
+                gn_store<T, V>(keep, to + (r + u * threads) * dx.row, k, f);
+            }
+        }
+    }
+}
+
+// dw and db of group blockIdx.y: the sum in fp64 of its `parts` partial sums, 32 channels per block, 8 threads to a channel.
+template <int>
+__global__ __launch_bounds__(kBlock) void k_gn_param_grads(const float* __restrict__ partial, int64_t parts, uint32_t C, LnParam dw, LnParam db) {
+    __shared__ double lds[8][32];
+    const LnParam& out = blockIdx.z ? db : dw;
+    if (!out.data) return;
+    const uint32_t col = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
+    const float* const p = partial + (size_t)blockIdx.y * parts * 2 * C + (blockIdx.z ? C : 0);
+    double sum = 0.0;
+    if (c < C) {
+#pragma unroll 4
+        for (int64_t q = slice; q < parts; q += 8) sum += (double)p[(size_t)q * 2 * C + c];
+    }
+    lds[slice][col] = sum;
+    __syncthreads();
+    if (slice == 0 && c < C) {
+        for (int q = 1; q < 8; ++q) sum += lds[q][col];
+        store_any(out.data, (int64_t)blockIdx.y * out.stride + c, out.type, (float)sum);
+    }
+}
+
+}  // namespace liec

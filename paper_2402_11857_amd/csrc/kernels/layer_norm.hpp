@@ -22,16 +22,6 @@ namespace liec {
 constexpr int kLnShortest = 8;         // columns of the shortest row that a team holds
 constexpr int kLnWide = 1024;          // threads that walk a row too long (or too short) for registers
 
-struct LnRows {                        // a [workers, rows, columns] tensor of unit column stride
-    void* data;
-    int64_t worker, row;               // strides, in elements
-};
-struct LnParam {                       // a [workers, columns] tensor of unit column stride; stride 0: one row for all workers
-    void* data;
-    int64_t stride;
-    uint32_t type;
-};
-
 // ---- sums over a team --------------------------------------------------------------------------------------------
 template <int CTRL>
 __device__ __forceinline__ float dpp_move(float v) {

@@ -11,13 +11,12 @@
 
 #include "kernels/grads.hpp"
 #include "kernels/layer_norm.hpp"
-#include "spans.hpp"
+#include "operands.hpp"
 
 using namespace liec;
 
 namespace {
 
-constexpr int32_t kMaxWorkers = 65535;
 constexpr int64_t kMaxGradValues = (int64_t)1 << 35;
 // Thread blocks of a launch that adds up squares, 16 per compute unit; six of them are resident at a time (norm of 16 x 11.7M
 // fp32 values: 2048 blocks 123 us, 4096 114).
@@ -30,12 +29,6 @@ constexpr int64_t kGradParts = 1024;
 // against 783 to 806 us, 220 MB 1790 against 1748 to 1798, 270 MB 2180 against 2169 to 2230, 330 MB 2648 against 2664 to 2738; into
 // rows 100 MB 1049 against 1122 to 1141, 270 MB 2746 against 3169 to 3241.  Rows would gain from 140 MB on (4 workers: 352 against 364).
 constexpr int64_t kGradRowBytes = (int64_t)256 << 20;
-
-bool valid_type(int t) { return t == LIEC_F32 || t == LIEC_BF16 || t == LIEC_F16; }
-int64_t size_of(int t) { return t == LIEC_F32 ? 4 : 2; }
-bool aligned_to(const void* p, int64_t size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) == 0; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-liec_status launched() { return hipGetLastError() == hipSuccess ? LIEC_OK : LIEC_EDEVICE; }
 
 // ---- gradients -------------------------------------------------------------------------------------------------------
 // Launches that T tensors take, at most.
@@ -59,8 +52,6 @@ bool valid_grads(const liec_grad_tensor* t, int32_t T, int32_t N, int64_t* total
     *total = sum;
     return true;
 }
-
-bool valid_workspace(const void* ws, int64_t bytes, int64_t need) { return ws && aligned_to(ws, 16) && bytes >= need; }
 
 // Where worker 0's values to worker N - 1's of a tensor lie.
 Span span_of_grads(const liec_grad_tensor& t, int32_t N) {
@@ -278,40 +269,6 @@ Strips backward_strips(int32_t N, int64_t R, int64_t C) {
     return {per, ceil_div(R, per)};
 }
 
-constexpr int64_t kMostValues = (int64_t)1 << 40;
-bool in_range(int64_t stride) { return stride >= -kMostValues && stride <= kMostValues; }
-bool valid_rows(const liec_rows* r, int32_t N, int64_t R, int64_t size) {
-    if (!r || !r->data || !aligned_to(r->data, size) || !in_range(r->worker_stride) || !in_range(r->row_stride)) return false;
-    return (double)(R - 1) * (double)llabs(r->row_stride) + (double)(N - 1) * (double)llabs(r->worker_stride) <= (double)kMostValues;
-}
-bool valid_param(const liec_param* p, int64_t size) { return !p || !p->data || (aligned_to(p->data, size) && in_range(p->stride)); }
-// Rows that are written must not share memory: the wider of the two strides spans what the narrower one covers.
-bool apart(const liec_rows* r, int32_t N, int64_t R, int64_t C) {
-    int64_t s = llabs(r->row_stride), n = R, wide = llabs(r->worker_stride), many = N;
-    if (many == 1 || (n > 1 && wide < s)) {
-        std::swap(s, wide);
-        std::swap(n, many);
-    }
-    return (n == 1 || s >= C) && (many == 1 || wide >= (n - 1) * s + C);
-}
-bool same(const liec_rows* a, const liec_rows* b, int32_t N, int64_t R) {
-    return a->data == b->data && (N == 1 || a->worker_stride == b->worker_stride) && (R == 1 || a->row_stride == b->row_stride);
-}
-Span span_of_rows(const liec_rows* r, int32_t N, int64_t R, int64_t C, int64_t size) {
-    return span_of(r->data, C * size, r->row_stride * size, R, r->worker_stride * size, N);
-}
-// An output may be an input, and must not share memory with it otherwise.
-bool may_write(const liec_rows* out, const liec_rows* in, int32_t N, int64_t R, int64_t C, int64_t size) {
-    return same(out, in, N, R) || !spans_meet(span_of_rows(out, N, R, C, size), span_of_rows(in, N, R, C, size));
-}
-Span span_of_param(const liec_param* p, int32_t N, int64_t C, int64_t size) {
-    return p && p->data ? span_of(p->data, C * size, p->stride * size, N) : Span();
-}
-// A weight gradient may take the place of the weight, row by row: a block has read what it replaces.
-bool may_replace(const liec_param* out, const liec_param* in, int32_t N, int64_t C, int64_t size) {
-    if (in && out && in->data && in->data == out->data && (N == 1 || in->stride == out->stride)) return true;
-    return !spans_meet(span_of_param(out, N, C, size), span_of_param(in, N, C, size));
-}
 LnRows rows_of(const liec_rows* r) { return r ? LnRows{r->data, r->worker_stride, r->row_stride} : LnRows{nullptr, 0, 0}; }
 LnParam param_of(const liec_param* p, int type) { return p && p->data ? LnParam{p->data, p->stride, (uint32_t)type} : LnParam{nullptr, 0, (uint32_t)type}; }
 
