@@ -209,7 +209,7 @@ bool valid_weight(int64_t N, int64_t R, int64_t O, int64_t C) {
     return n * (double)O * (double)C <= most && n * (double)R * (double)O <= most && n * (double)R * (double)C <= most;
 }
 
-int64_t wg_tile(int64_t O, int64_t C) { return O > 64 && C > 64 ? 128 : 64; }
+int64_t wg_tile(int64_t O, int64_t C) { return O > 128 && C > 128 ? 256 : O > 64 && C > 64 ? 128 : 64; }
 
 WgShape weight_shape(int64_t N, int64_t R, int64_t O, int64_t C) {
     WgShape s{};
@@ -227,8 +227,15 @@ WgShape weight_shape(int64_t N, int64_t R, int64_t O, int64_t C) {
 template <typename T>
 void weight_grad_of(const WgShape& s, const LnRows& dy, const Saved& x, const WgOut& dw, const LnParam& db, float* partial, hipStream_t st) {
     const uint32_t grid = grid_of((int64_t)s.N * s.splits * s.tiles_o * s.tiles_c);
-    constexpr int BK = sizeof(T) == 4 ? 32 : 64;
-    if (wg_tile(s.O, s.C) == 128) k_weight_grad<T, 128, 128, BK, 2, 2><<<grid, 256, 0, st>>>(s, dy, x, dw, db, partial);
+    constexpr int BK = Parts<T>::n == 1 ? 64 : 32;
+    const int64_t step = BK * std::max(dy.row * (int64_t)sizeof(T), s.C);
+    const bool aligned = ((uintptr_t)dy.data | (uintptr_t)x.q) % 16 == 0 && (dy.row | dy.worker) * (int64_t)sizeof(T) % 16 == 0 && s.C % 16 == 0 && dy.row >= s.O &&
+                         step < (int64_t)1 << 30 && s.R;
+    const int64_t tile = wg_tile(s.O, s.C);
+    if (aligned && tile == 256) k_weight_grad_aligned<T, 256, 256, BK, 4, 2><<<grid, 512, 0, st>>>(s, dy, x, dw, db, partial);
+    else if (aligned && tile == 128) k_weight_grad_aligned<T, 128, 128, BK, 2, 2><<<grid, 256, 0, st>>>(s, dy, x, dw, db, partial);
+    else if (tile == 256) k_weight_grad<T, 256, 256, BK, 4, 2><<<grid, 512, 0, st>>>(s, dy, x, dw, db, partial);
+    else if (tile == 128) k_weight_grad<T, 128, 128, BK, 2, 2><<<grid, 256, 0, st>>>(s, dy, x, dw, db, partial);
     else k_weight_grad<T, 64, 64, 64, 2, 2><<<grid, 256, 0, st>>>(s, dy, x, dw, db, partial);
     if (partial) k_weight_grad_join<0><<<dim3(grid_of(ceil_div(s.O * (s.C + 1), kBlock)), s.N), kBlock, 0, st>>>(s, partial, dw, db);
 }

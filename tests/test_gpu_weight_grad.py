@@ -52,7 +52,8 @@ def _check(dy, saved, dw, db):
 # both sides of every change of tiles, splits and steps; lengths of no vector; one row, one column
 SIZES = [(1, 1, 1, 1), (2, 1, 5, 33), (3, 2, 64, 64), (2, 7, 65, 63), (4, 32, 10, 160), (1, 63, 100, 31), (2, 64, 128, 128), (1, 65, 129, 127), (2, 300, 130, 257),
          (1, 1000, 17, 1001), (3, 129, 1, 300), (1, 257, 300, 1), (1, 8193, 40, 72), (1, 20_001, 70, 66), (5, 255, 96, 80), (1, 640, 512, 520), (2, 100, 385, 511), (70, 9, 12, 20),
-         (1, 4100, 256, 264), (2, 513, 1030, 90), (1, 90, 90, 2050)]
+         (1, 4100, 256, 264), (2, 513, 1030, 90), (1, 90, 90, 2050),
+         (2, 333, 272, 304), (1, 129, 136, 144), (3, 200, 520, 400), (1, 8200, 264, 272), (2, 64, 72, 1008), (1, 1, 512, 512), (9, 65, 256, 256)]
 
 
 @pytest.mark.parametrize("N,R,O,C", SIZES)
@@ -83,7 +84,7 @@ def test_types_and_strides(dtype, params):
     import paper_2402_11857_amd as pkg
 
     say(f"case weight gradient strides {dtype} {params}")
-    for N, R, O, C in ((3, 50, 40, 70), (2, 9000, 33, 17)):
+    for N, R, O, C in ((3, 50, 40, 70), (2, 9000, 33, 17), (2, 150, 133, 144), (2, 90, 75, 80)):
         dy, saved = _inputs(N, R, O, C, dtype, seed=5)
         room = torch.full((N, O + 3, C + 5), 4.0, dtype=DTYPES[params], device=DEV)
         dw, bias = room[:, 1:1 + O, 2:2 + C], torch.full((N, O + 9), 4.0, dtype=DTYPES[params], device=DEV)
@@ -98,6 +99,12 @@ def test_types_and_strides(dtype, params):
         view = wide[:, ::2, 5:5 + O]
         view.copy_(dy)
         assert torch.equal(pkg.liec_weight_grad(view, saved), pkg.liec_weight_grad(dy, saved))
+        # rows at distances of 16 bytes that are longer than dy, or overlap
+        room = torch.full((N, R, 8 * (O // 8 + 2)), float("nan"), dtype=dy.dtype, device=DEV)
+        room[..., 8:8 + O] = dy
+        assert torch.equal(pkg.liec_weight_grad(room[..., 8:8 + O], saved), pkg.liec_weight_grad(dy, saved))
+        near = torch.randn(N, R * 16 + O, generator=generator(6), device=DEV).to(dy.dtype).as_strided((N, R, O), (R * 16 + O, 16, 1))
+        assert torch.equal(pkg.liec_weight_grad(near, saved), pkg.liec_weight_grad(near.contiguous(), saved))
         same = dy[:1].expand(N, R, O)
         assert torch.equal(pkg.liec_weight_grad(same, saved), pkg.liec_weight_grad(same.contiguous(), saved))
 
