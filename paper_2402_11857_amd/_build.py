@@ -14,7 +14,7 @@ SOURCES = [os.path.join(_HERE, "csrc", n) for n in ("liec_api.hip", "train_api.h
 HEADERS = [os.path.join(_HERE, "csrc", n) for n in ("liec_kernels.hpp", "operands.hpp", "spans.hpp")] + \
           [os.path.join(_ROOT, "include", n) for n in ("liec.h", "liec_testing.h", "liec_train.h", "liec_activations.h")] + \
           [os.path.join(_HERE, "csrc", "kernels", n)
-           for n in ("checkpoint.hpp", "common.hpp", "elements.hpp", "grads.hpp", "group_norm.hpp", "layer_norm.hpp", "rows.hpp", "select.hpp", "sign.hpp",
+           for n in ("checkpoint.hpp", "common.hpp", "elements.hpp", "grads.hpp", "group_norm.hpp", "group_norm_held.hpp", "layer_norm.hpp", "rows.hpp", "select.hpp", "sign.hpp",
                      "step.hpp", "sync.hpp", "telemetry.hpp", "weight_grad.hpp", "wire.hpp")]
 
 

@@ -6,7 +6,7 @@
 
 #include <algorithm>
 
-#include "kernels/group_norm.hpp"
+#include "kernels/group_norm_held.hpp"
 #include "kernels/weight_grad.hpp"
 #include "operands.hpp"
 
@@ -117,7 +117,7 @@ bool valid_norm(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
     return (double)N * (double)B * (double)std::max<int64_t>(S, 1) * (double)C <= (double)kMostValues;
 }
 
-constexpr int64_t kGnBlocks = 4096;    // that a launch should have at least, where there is work for them
+constexpr int64_t kGnBlocks = 2048;    // that a launch should have at least, where there is work for them
 constexpr int64_t kGnChain = 256;      // positions that a thread adds up
 
 int log_of(int64_t n) {                // of the next power of two
@@ -129,7 +129,7 @@ int log_of(int64_t n) {                // of the next power of two
 GnShape shape_of(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
     GnShape s{};
     const int64_t pieces = C < 8 ? C : ceil_div(C, 8);
-    s.images = N * B, s.B = B, s.S = S, s.C = (uint32_t)C, s.G = (uint32_t)G, s.per_group = (uint32_t)(C / G);
+    s.images = N * B, s.B = B, s.S = S, s.C = (uint32_t)C, s.G = (uint32_t)G, s.per_group = (uint32_t)(C / G), s.whole = C / G % 8 == 0;
     // four lanes at least where a row is not shorter: those that share an exponent of a checkpoint
     s.lanes_log = (uint32_t)std::min(6, C < 8 ? log_of(C) : std::max(2, log_of(pieces)));
     s.tiles = (uint32_t)ceil_div(pieces, (int64_t)1 << s.lanes_log);
@@ -145,6 +145,45 @@ uint32_t gn_group_blocks(const GnShape& s) { return grid_of(ceil_div(s.images * 
 int64_t gn_partials(const GnShape& s) { return s.images * s.splits * 2 * (int64_t)s.C; }
 GnImages images_of(const liec_images* x) { return x && x->data ? GnImages{x->data, x->worker_stride, x->image_stride, x->row_stride} : GnImages{nullptr, 0, 0, 0}; }
 
+// Does a block hold a group's positions, `most` of them per thread?  Spans of `wide` bytes per position if they fit, then half and a
+// quarter of that, in multiples of `least` channels (those that share an exponent of a checkpoint, or a vector); rows whose groups do
+// not come to that are taken whole.
+bool hold(const GnShape& s, int64_t size, int64_t most, int64_t least, GnHeld* h) {
+    const int64_t pg = s.per_group, C = s.C;
+    if (C < 8 || s.S > most * kGnHeldMost) return false;
+    for (int64_t wide = 128; wide >= 32; wide /= 2) {
+        int64_t groups = ceil_div(wide / size, pg);
+        while (groups < s.G && groups * pg % least) ++groups;
+        h->span = (uint32_t)std::min(groups * pg, C);
+        h->spans = (uint32_t)ceil_div(C, (int64_t)h->span);
+        h->lanes_log = (uint32_t)std::max(log_of(ceil_div(h->span, 8)), log_of(least / 8));
+        if (h->lanes_log > 6) continue;
+        h->rows_log = (uint32_t)log_of(ceil_div(s.S, most));
+        while (h->lanes_log + h->rows_log < 8 && ((int64_t)1 << h->rows_log) < s.S) ++h->rows_log;
+        if (((int64_t)1 << (h->lanes_log + h->rows_log)) > kGnHeldMost) continue;
+        // more images where one is small: of one worker, so as many as its number of them is a multiple of
+        h->images_log = 0;
+        while (h->lanes_log + h->rows_log + h->images_log < 8 && s.B % ((int64_t)2 << h->images_log) == 0) ++h->images_log;
+        while (h->lanes_log + h->rows_log + h->images_log < 6) ++h->rows_log;          // whole waves
+        h->rows = (uint32_t)ceil_div(s.S, (int64_t)1 << h->rows_log);
+        return true;
+    }
+    return false;
+}
+// An operand whose values a block finds at distances of less than 2^31 bytes.
+bool near(const GnImages& x, const GnShape& s, const GnHeld& h, int64_t size) {
+    if (x.image < 0 || x.row < 0) return false;
+    return ((double)(((int64_t)1 << h.images_log) - 1) * (double)x.image + (double)s.S * (double)x.row + (double)s.C) * (double)size < 2147483648.0;
+}
+int64_t held_threads(const GnHeld& h) { return (int64_t)1 << (h.lanes_log + h.rows_log + h.images_log); }
+int64_t held_waves(const GnHeld& h) { return h.lanes_log + h.rows_log > 6 ? (int64_t)1 << (h.lanes_log + h.rows_log - 6) : 1; }
+constexpr int64_t kGnHeldBytes = 64 << 10;                           // of LDS
+int64_t held_bytes(const GnShape& s, const GnHeld& h, bool backward) {
+    const int64_t entries = !backward && s.whole ? h.span / 8 : h.span, images = (int64_t)1 << h.images_log;
+    return 4 * images * (2 * entries * held_waves(h) + (backward ? 2 * (int64_t)h.span : 0) + 2 * (h.span / s.per_group));
+}
+uint32_t held_grid(const GnShape& s, const GnHeld& h) { return grid_of((s.images >> h.images_log) * h.spans); }
+
 struct GnForward {
     GnShape s;
     GnImages x, y;
@@ -156,16 +195,34 @@ struct GnForward {
     hipStream_t st;
 };
 
+template <typename T, int K, int ACT>
+void gn_held_of(const GnForward& a, const GnHeld& h) {
+    const auto f = a.saved.q ? k_gn_held<T, K, ACT, true> : k_gn_held<T, K, ACT, false>;
+    f<<<held_grid(a.s, h), (uint32_t)held_threads(h), (size_t)held_bytes(a.s, h, false), a.st>>>(a.s, h, a.keep, a.eps, a.mean, a.rstd, a.x, a.y, a.w, a.b, a.saved);
+}
+template <typename T, int K>
+void gn_held_of(const GnForward& a, const GnHeld& h) {
+    a.act == kActNone ? gn_held_of<T, K, kActNone>(a, h) : a.act == kActRelu ? gn_held_of<T, K, kActRelu>(a, h) : gn_held_of<T, K, kActSilu>(a, h);
+}
+
 template <typename T, int V>
 void gn_forward_of(const GnForward& a) {
     const uint32_t grid = grid_of(gn_works_of(a.s));
     k_gn_stats<T, V><<<grid, kBlock, 0, a.st>>>(a.s, a.x, a.partial);
     k_gn_groups<0><<<gn_group_blocks(a.s), kBlock, 0, a.st>>>(a.s, a.partial, a.eps, a.mean, a.rstd);
-    const auto apply = a.act == kActNone ? k_gn_apply<T, V, kActNone> : a.act == kActRelu ? k_gn_apply<T, V, kActRelu> : k_gn_apply<T, V, kActSilu>;
+    const auto apply = a.saved.q ? (a.act == kActNone ? k_gn_apply<T, V, kActNone, true> : a.act == kActRelu ? k_gn_apply<T, V, kActRelu, true> : k_gn_apply<T, V, kActSilu, true>)
+                                 : (a.act == kActNone ? k_gn_apply<T, V, kActNone, false> : a.act == kActRelu ? k_gn_apply<T, V, kActRelu, false> : k_gn_apply<T, V, kActSilu, false>);
     apply<<<grid, kBlock, 0, a.st>>>(a.s, a.keep, a.mean, a.rstd, a.x, a.y, a.w, a.b, a.saved);
 }
+// Positions of a thread in registers: 128 of those for values.
 template <typename T>
-void gn_forward_of(const GnForward& a) { a.s.C < 8 ? gn_forward_of<T, 1>(a) : gn_forward_of<T, 8>(a); }
+void gn_forward_of(const GnForward& a) {
+    constexpr int most = sizeof(T) == 2 ? 32 : 16;
+    GnHeld h;
+    if (hold(a.s, sizeof(T), most, kSavedCols, &h) && held_bytes(a.s, h, false) <= kGnHeldBytes && near(a.x, a.s, h, sizeof(T)) && near(a.y, a.s, h, sizeof(T)))
+        h.rows <= most / 4 ? gn_held_of<T, most / 4>(a, h) : gn_held_of<T, most>(a, h);
+    else a.s.C < 8 ? gn_forward_of<T, 1>(a) : gn_forward_of<T, 8>(a);
+}
 
 struct GnBackward {
     GnShape s;
@@ -177,6 +234,18 @@ struct GnBackward {
     bool keep;
     hipStream_t st;
 };
+
+template <typename T, int K, int ACT, bool SAVED>
+void gn_held_of(const GnBackward& a, const GnHeld& h) {
+    k_gn_held_backward<T, K, ACT, SAVED><<<held_grid(a.s, h), (uint32_t)held_threads(h), (size_t)held_bytes(a.s, h, true), a.st>>>(
+        a.s, h, a.keep, a.mean, a.rstd, a.dy, a.x, a.saved, a.dx, a.w, a.b, a.partial);
+}
+template <typename T, int K, int ACT>
+void gn_held_of(const GnBackward& a, const GnHeld& h) { a.saved.q ? gn_held_of<T, K, ACT, true>(a, h) : gn_held_of<T, K, ACT, false>(a, h); }
+template <typename T, int K>
+void gn_held_of(const GnBackward& a, const GnHeld& h, int act) {
+    act == kActNone ? gn_held_of<T, K, kActNone>(a, h) : act == kActRelu ? gn_held_of<T, K, kActRelu>(a, h) : gn_held_of<T, K, kActSilu>(a, h);
+}
 
 template <typename T, int V, int ACT, bool SAVED>
 void gn_backward_of(const GnBackward& a) {
@@ -193,8 +262,19 @@ template <typename T, int V>
 void gn_backward_of(const GnBackward& a, int act) {
     act == kActNone ? gn_backward_of<T, V, kActNone>(a) : act == kActRelu ? gn_backward_of<T, V, kActRelu>(a) : gn_backward_of<T, V, kActSilu>(a);
 }
+// Returns the number of partial sums of all images.
 template <typename T>
-void gn_backward_of(const GnBackward& a, int act) { a.s.C < 8 ? gn_backward_of<T, 1>(a, act) : gn_backward_of<T, 8>(a, act); }
+int64_t gn_backward_of(const GnBackward& a, int act) {
+    constexpr int most = sizeof(T) == 2 ? 16 : 8;
+    GnHeld h;
+    if (hold(a.s, sizeof(T), most, 8, &h) && held_bytes(a.s, h, true) <= kGnHeldBytes && near(a.x, a.s, h, sizeof(T)) && near(a.dy, a.s, h, sizeof(T)) &&
+        near(a.dx, a.s, h, sizeof(T)) && near(GnImages{nullptr, 0, a.s.S * (int64_t)a.s.C, a.s.C}, a.s, h, 1)) {
+        h.rows <= most / 4 ? gn_held_of<T, most / 4>(a, h, act) : gn_held_of<T, most>(a, h, act);
+        return a.s.images >> h.images_log;
+    }
+    a.s.C < 8 ? gn_backward_of<T, 1>(a, act) : gn_backward_of<T, 8>(a, act);
+    return a.s.images * a.s.splits;
+}
 
 bool valid_act(int a) { return a == LIEC_ACT_NONE || a == LIEC_ACT_RELU || a == LIEC_ACT_SILU; }
 
@@ -365,14 +445,12 @@ liec_status liec_group_norm_backward(const liec_images* dy, const liec_images* x
     GnBackward a{shape_of(N, B, S, C, G), images_of(dy), images_of(x), images_of(dx), saved_of(saved), param_of(weight, param_dtype), param_of(bias, param_dtype),
                  param_of(dweight, param_dtype), param_of(dbias, param_dtype), mean, rstd, static_cast<float*>(workspace),
                  keeps((int64_t)N * B * S * C * size), st};
-    if (!empty && (dx || dweight || dbias)) {
-        if (dtype == LIEC_F32) gn_backward_of<float>(a, activation);
-        else if (dtype == LIEC_BF16) gn_backward_of<bf16>(a, activation);
-        else gn_backward_of<f16>(a, activation);
-    }
+    int64_t parts = 0;
+    if (!empty && (dx || dweight || dbias))
+        parts = dtype == LIEC_F32 ? gn_backward_of<float>(a, activation) : dtype == LIEC_BF16 ? gn_backward_of<bf16>(a, activation) : gn_backward_of<f16>(a, activation);
     if (dweight || dbias) {
         const bool shared = N == 1 || (dweight ? dweight : dbias)->stride == 0;
-        const int64_t parts = empty ? 0 : (shared ? a.s.images : B) * (int64_t)a.s.splits;
+        if (!shared) parts /= N;
         k_gn_param_grads<0><<<dim3((uint32_t)ceil_div(C, 32), shared ? 1u : (uint32_t)N, 2), kBlock, 0, st>>>(a.partial, parts, (uint32_t)C, a.dw, a.db);
     }
     return launched();

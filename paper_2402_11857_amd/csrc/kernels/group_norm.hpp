@@ -27,40 +27,37 @@ struct GnShape {
     int64_t images, B, S;              // images = N * B
     uint32_t C, G, per_group;
     uint32_t lanes_log;                // a row-thread's lanes, each with 8 channels (one, where C < 8): tiles of the channels
+    bool whole;                        // groups are a multiple of 8 channels
     uint32_t tiles, splits;            // a block's work: one tile, `per` of an image's positions
     int64_t per;
 };
 
 // ---- activation ------------------------------------------------------------------------------------------------------
-// exp(-z) with the product's rounding error put right, to about 2 u; at most 2^126, so that its reciprocal is a number.
+// exp(-z), at most 2^126.  For results of 16 bits the product's rounding error stays, |z| u of the exponential; for fp32 it is put
+// right, to about 2 u.
+template <typename T>
 __device__ __forceinline__ float exp_minus(float z) {
     const float log2e = 1.44269502f, rest = 1.92596299e-8f;              // their sum is log2(e)
-    const float t = -z * log2e, off = __fmaf_rn(-z, rest, __fmaf_rn(-z, log2e, -t));
-    const float e = __builtin_amdgcn_exp2f(fminf(t, 126.f));
+    const float t = -z * log2e, e = __builtin_amdgcn_exp2f(fminf(t, 126.f));
+    if (sizeof(T) == 2) return e;
+    const float off = __fmaf_rn(-z, rest, __fmaf_rn(-z, log2e, -t));
     return fabsf(t) < 126.f ? __fmaf_rn(e, off * 0.693147181f, e) : e;
 }
 
-template <int ACT>
+template <typename T, int ACT>
 __device__ __forceinline__ float act_of(float z) {
     if (ACT == kActRelu) return z < 0.f ? 0.f : z;
-    if (ACT == kActSilu) return z * __builtin_amdgcn_rcpf(1.f + exp_minus(z));
+    if (ACT == kActSilu) return z * __builtin_amdgcn_rcpf(1.f + exp_minus<T>(z));
     return z;
 }
 
-// dz and h of a value.  The sign of z decides a ReLU's gradient: in fp32 z is off by at most 2 u |h w| + u |z|, so it is right unless
-// |z| <= 4 u |b| (then |h w| <= |b| (1 + 4 u)), and such a value is looked at in fp64.
-template <int ACT>
-__device__ __forceinline__ float dz_of(float dy, float x, float mu, float rs, float w, float b, float& h) {
-    h = (x - mu) * rs;
+// dz from dy and z.
+template <typename T, int ACT>
+__device__ __forceinline__ float dz_of(float dy, float z) {
     if (ACT == kActNone) return dy;
-    const float z = __fmaf_rn(h, w, b);
-    if (ACT == kActRelu) {
-        bool on = z > 0.f;
-        if (__builtin_expect(fabsf(z) <= 0x1p-22f * fabsf(b), 0)) on = ((double)x - (double)mu) * (double)rs * (double)w + (double)b > 0.0;
-        return on ? dy : 0.f;
-    }
-    const float e = exp_minus(z), p = __builtin_amdgcn_rcpf(1.f + e);
-    return dy * (p * __fmaf_rn(z, e * p, 1.f));                          // p (1 + z (1 - p)),  1 - p = e p
+    if (ACT == kActRelu) return z > 0.f ? dy : 0.f;
+    const float p = __builtin_amdgcn_rcpf(1.f + exp_minus<T>(z));
+    return dy * (p * __fmaf_rn(z, 1.f - p, 1.f));                        // p (1 + z (1 - p))
 }
 
 // ---- a thread's channels ----------------------------------------------------------------------------------------------
@@ -82,18 +79,39 @@ __device__ __forceinline__ GnColumns gn_columns(const GnShape& s, uint32_t tile,
 template <typename T, int V, bool SAVED>
 struct GnRaw {
     Eight<T> v;
+    // What comes before and after does not share widened values, which take up to four times the registers.
+    __device__ __forceinline__ void hide() {
+#pragma unroll
+        for (int i = 0; i < Eight<T>::words; ++i) asm volatile("" : "+v"(v.w[i]));
+    }
     __device__ __forceinline__ void load(const T* row, const GnColumns& k) { v = ld_eight<T, false>(row + k.c); }
     __device__ __forceinline__ void widen(const GnColumns&, float (&f)[V]) const { widen_eight<T>(v, f); }
+    __device__ __forceinline__ void narrow(const float (&f)[V]) {
+#pragma unroll
+        for (int i = 0; i < Eight<T>::words; ++i) {
+            float part[Vec16<T>::n];
+#pragma unroll
+            for (int j = 0; j < Vec16<T>::n; ++j) part[j] = f[i * Vec16<T>::n + j];
+            v.w[i] = Vec16<T>::narrow(part);
+        }
+    }
+    __device__ __forceinline__ void center(const GnColumns& k, const float (&mu)[V], float (&f)[V]) const {
+        widen(k, f);
+#pragma unroll
+        for (int j = 0; j < V; ++j) f[j] -= mu[j];
+    }
 };
 template <typename T>
 struct GnRaw<T, 1, false> {
     T v;
     __device__ __forceinline__ void load(const T* row, const GnColumns& k) { v = row[k.c]; }
     __device__ __forceinline__ void widen(const GnColumns&, float (&f)[1]) const { f[0] = liec::widen(v); }
+    __device__ __forceinline__ void center(const GnColumns&, const float (&mu)[1], float (&f)[1]) const { f[0] = liec::widen(v) - mu[0]; }
 };
 template <typename T>
 struct GnRaw<T, 8, true> {
     v2u w;
+    __device__ __forceinline__ void hide() { asm volatile("" : "+v"(w), "+v"(e)); }
     uint32_t e;                        // the last channel's exponent, and that of every channel that is not left out
     __device__ __forceinline__ void load(const Saved& s, int64_t row, uint32_t C, uint32_t groups, const GnColumns& k) {
         w = ld8_bytes(s.q + row * C + k.c);
@@ -102,6 +120,12 @@ struct GnRaw<T, 8, true> {
     __device__ __forceinline__ void widen(const GnColumns&, float (&f)[8]) const {
         unpack4(w.x, saved_scale(e), f);
         unpack4(w.y, saved_scale(e), f + 4);
+    }
+    // x - mu with one rounding: q 2^k is exact
+    __device__ __forceinline__ void center(const GnColumns&, const float (&mu)[8], float (&f)[8]) const {
+        const float scale = saved_scale(e);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = __fmaf_rn((float)(int8_t)((j < 4 ? w.x : w.y) >> (8 * (j & 3))), scale, -mu[j]);
     }
 };
 template <typename T>
@@ -113,13 +137,19 @@ struct GnRaw<T, 1, true> {
         e = s.e[row * groups];
     }
     __device__ __forceinline__ void widen(const GnColumns&, float (&f)[1]) const { f[0] = (float)q * saved_scale(e); }
+    __device__ __forceinline__ void center(const GnColumns&, const float (&mu)[1], float (&f)[1]) const { f[0] = __fmaf_rn((float)q, saved_scale(e), -mu[0]); }
 };
 
+__device__ __forceinline__ int64_t gn_worker(const GnShape& s, int64_t image) {
+    return s.images <= 0x7fffffff ? (int64_t)((uint32_t)image / (uint32_t)s.B) : image / s.B;
+}
 template <typename T>
 __device__ __forceinline__ T* gn_image(const GnImages& m, const GnShape& s, int64_t image) {
-    const int64_t worker = image / s.B;
+    const int64_t worker = gn_worker(s, image);
     return static_cast<T*>(m.data) + worker * m.worker + (image - worker * s.B) * m.image;
 }
+
+__device__ __forceinline__ int64_t gn_works(const GnShape& s) { return s.images * s.splits * s.tiles; }
 
 struct GnWork {
     uint32_t tile, split;
@@ -127,15 +157,21 @@ struct GnWork {
 };
 __device__ __forceinline__ GnWork gn_work(const GnShape& s, int64_t work) {
     GnWork r;
-    const int64_t strip = work / s.tiles;
-    r.tile = (uint32_t)(work - strip * s.tiles);
-    r.image = strip / s.splits;
-    r.split = (uint32_t)(strip - r.image * s.splits);
+    if (gn_works(s) <= 0x7fffffff) {   // a division of 64 bits takes some 150 instructions
+        const uint32_t strip = (uint32_t)work / s.tiles, image = strip / s.splits;
+        r.tile = (uint32_t)work - strip * s.tiles;
+        r.split = strip - image * s.splits;
+        r.image = image;
+    } else {
+        const int64_t strip = work / s.tiles;
+        r.tile = (uint32_t)(work - strip * s.tiles);
+        r.image = strip / s.splits;
+        r.split = (uint32_t)(strip - r.image * s.splits);
+    }
     r.first = r.split * s.per;
     r.end = min(r.first + s.per, s.S);
     return r;
 }
-__device__ __forceinline__ int64_t gn_works(const GnShape& s) { return s.images * s.splits * s.tiles; }
 
 constexpr int kGnAhead = 4;            // positions of a thread requested together
 constexpr int kGnTile = 512;           // channels of a tile, at most
@@ -318,26 +354,58 @@ __device__ __forceinline__ void gn_save(const Saved& out, int64_t row, const GnS
     }
 }
 
+// V neighbouring parameters of a worker.
+template <int V>
+__device__ __forceinline__ void gn_param(const LnParam& p, int64_t worker, uint32_t c, float none, float (&f)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = none;
+    if (!p.data) return;
+    const int64_t at = worker * p.stride + c;
+    if constexpr (V == 8) {
+        if (p.type == kF32) widen_eight<float>(ld_eight<float, false>(static_cast<const float*>(p.data) + at), f);
+        else if (p.type == kBF16) widen_eight<bf16>(ld_eight<bf16, false>(static_cast<const bf16*>(p.data) + at), f);
+        else widen_eight<f16>(ld_eight<f16, false>(static_cast<const f16*>(p.data) + at), f);
+    } else {
+        f[0] = load_any(p.data, at, p.type);
+    }
+}
+// The groups of V neighbouring channels: f(j, group), in order.
+template <int V, typename F>
+__device__ __forceinline__ void gn_each_group(const GnShape& s, uint32_t c, F f) {
+    uint32_t g = c / s.per_group, left = (g + 1) * s.per_group - c;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        f(j, g);
+        if (--left == 0) {
+            ++g;
+            left = s.per_group;
+        }
+    }
+}
+
 template <int V>
 struct GnParams {
     float mu[V], rs[V], w[V], b[V];
     __device__ __forceinline__ void load(const GnShape& s, int64_t image, const GnColumns& k, const float* mean, const float* rstd, const LnParam& weight,
                                          const LnParam& bias) {
-        const int64_t worker = image / s.B;
+        const int64_t worker = gn_worker(s, image);
+        const uint32_t c = k.any ? k.c : 0u;
+        gn_param<V>(weight, worker, c, 1.f, w);
+        gn_param<V>(bias, worker, c, 0.f, b);
+        mean += image * s.G;
+        rstd += image * s.G;
+        if (V == 8 && s.whole) {       // one group for all eight
+            const uint32_t g = c / s.per_group;
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const uint32_t c = k.any ? k.c + j : 0u;
-            const int64_t g = image * s.G + c / s.per_group;
-            mu[j] = mean[g];
-            rs[j] = rstd[g];
-            w[j] = weight.data ? load_any(weight.data, worker * weight.stride + c, weight.type) : 1.f;
-            b[j] = bias.data ? load_any(bias.data, worker * bias.stride + c, bias.type) : 0.f;
+            for (int j = 0; j < V; ++j) mu[j] = mean[g], rs[j] = rstd[g];
+        } else {
+            gn_each_group<V>(s, c, [&](int j, uint32_t g) { mu[j] = mean[g], rs[j] = rstd[g]; });
         }
     }
 };
 
-// y, and the checkpoint of x where `out.q` is there.
-template <typename T, int V, int ACT>
+// y, and the checkpoint of x where SAVE.
+template <typename T, int V, int ACT, bool SAVE>
 __global__ __launch_bounds__(kBlock) void k_gn_apply(GnShape s, bool keep, const float* __restrict__ mean, const float* __restrict__ rstd, GnImages x, GnImages y,
                                                      LnParam weight, LnParam bias, Saved out) {
     const uint32_t lane = threadIdx.x & ((1u << s.lanes_log) - 1), thread = threadIdx.x >> s.lanes_log, threads = kBlock >> s.lanes_log;
@@ -362,10 +430,10 @@ __global__ __launch_bounds__(kBlock) void k_gn_apply(GnShape s, bool keep, const
                 if (u >= rows) break;
                 float f[V];
                 if (k.any) raw[u].widen(k, f);
-                if (out.q) gn_save<V>(out, w.image * s.S + r + u * threads, s, k, f);
+                if (SAVE) gn_save<V>(out, w.image * s.S + r + u * threads, s, k, f);
                 if (!k.any) continue;
 #pragma unroll
-                for (int j = 0; j < V; ++j) f[j] = act_of<ACT>(__fmaf_rn(f[j] - p.mu[j], p.rs[j], p.b[j]));
+                for (int j = 0; j < V; ++j) f[j] = act_of<T, ACT>(__fmaf_rn(f[j] - p.mu[j], p.rs[j], p.b[j]));
                 gn_store<T, V>(keep, to + (r + u * threads) * y.row, k, f);
             }
         }
@@ -373,6 +441,40 @@ __global__ __launch_bounds__(kBlock) void k_gn_apply(GnShape s, bool keep, const
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------------------
+// A ReLU's dz of a row with the signs of z in fp64.  One channel after the other, picked out here, so that these few rows do not set how
+// many registers all others take.
+template <int V, typename R, typename G>
+__device__ __forceinline__ void gn_dz_exact(float (&g)[V], const GnParams<V>& p, const R& raw, const G& grad, const GnColumns& k) {
+    float f[V];
+    raw.widen(k, f);
+    grad.widen(k, g);
+#pragma unroll 1
+    for (int j = 0; j < V; ++j) {
+        float x = 0.f, mu = 0.f, rs = 0.f, w = 0.f, b = 0.f;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i == j) x = f[i], mu = p.mu[i], rs = p.rs[i], w = p.w[i], b = p.b[i];
+        const bool on = ((double)x - (double)mu) * (double)rs * (double)w + (double)b > 0.0;
+#pragma unroll
+        for (int i = 0; i < V; ++i) g[i] = i == j && !on ? 0.f : g[i];
+    }
+}
+// dz of a thread's channels in the place of dy, with d = x - mu and zw = rstd w.  The sign of z = d zw + b decides a ReLU's gradient: in
+// fp32 z is off by at most 2 u |d zw| + u |z|, so it is right unless |z| <= 4 u |b| (then |d zw| <= |b| (1 + 4 u)).  Rows with such a
+// channel, a few in a million, are looked at again.
+template <typename T, int V, int ACT, typename R, typename G>
+__device__ __forceinline__ void gn_dz(float (&g)[V], const float (&d)[V], const float (&zw)[V], const GnParams<V>& p, const R& raw, const G& grad, const GnColumns& k) {
+    if (ACT == kActNone) return;
+    bool near = false;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const float z = __fmaf_rn(d[j], zw[j], p.b[j]);
+        if (ACT == kActRelu) near |= fabsf(z) <= 0x1p-22f * fabsf(p.b[j]);
+        g[j] = dz_of<T, ACT>(g[j], z);
+    }
+    if (ACT == kActRelu && __builtin_expect(near, 0)) gn_dz_exact<V>(g, p, raw, grad, k);
+}
+
 template <typename T, int V, bool SAVED>
 __device__ __forceinline__ void gn_load(GnRaw<T, V, SAVED>& raw, const T* image, const GnImages& x, const Saved& saved, const GnShape& s, const GnWork& w, int64_t r,
                                         const GnColumns& k) {
@@ -393,6 +495,9 @@ __global__ __launch_bounds__(kBlock) void k_gn_sums(GnShape s, const float* __re
         const T* const gs = gn_image<const T>(dy, s, w.image);
         GnParams<V> p;
         p.load(s, w.image, k, mean, rstd, weight, bias);
+        float zw[V];
+#pragma unroll
+        for (int j = 0; j < V; ++j) zw[j] = p.rs[j] * p.w[j];
         float sum_h[V], sum_1[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) sum_h[j] = sum_1[j] = 0.f;
@@ -409,17 +514,19 @@ __global__ __launch_bounds__(kBlock) void k_gn_sums(GnShape s, const float* __re
 #pragma unroll
             for (int u = 0; u < kGnAhead; ++u) {
                 if (u >= rows) break;
-                float f[V], g[V], h;
-                raw[u].widen(k, f);
+                float d[V], g[V];
+                raw[u].center(k, p.mu, d);
                 grad[u].widen(k, g);
+                gn_dz<T, V, ACT>(g, d, zw, p, raw[u], grad[u], k);
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    const float dz = dz_of<ACT>(g[j], f[j], p.mu[j], p.rs[j], p.w[j], p.b[j], h);
-                    sum_1[j] += dz;
-                    sum_h[j] = __fmaf_rn(dz, h, sum_h[j]);
+                    sum_1[j] += g[j];
+                    sum_h[j] = __fmaf_rn(g[j], d[j], sum_h[j]);
                 }
             }
         }
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum_h[j] *= p.rs[j];
         for (uint32_t off = 1u << s.lanes_log; off < 64; off <<= 1) {
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -479,9 +586,14 @@ __global__ __launch_bounds__(kBlock) void k_gn_dx(GnShape s, bool keep, const fl
         T* const to = gn_image<T>(dx, s, w.image);
         GnParams<V> p;
         p.load(s, w.image, k, mean, rstd, weight, bias);
-        float2 m[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) m[j] = means[w.image * s.G + (k.c + j) / s.per_group];
+        // dx = rs (dz w - m1 - d rs m2) = dz zw - (d k2 + k1)
+        float zw[V], k1[V], k2[V];
+        gn_each_group<V>(s, k.c, [&](int j, uint32_t g) {
+            const float2 m = means[w.image * s.G + g];
+            zw[j] = p.rs[j] * p.w[j];
+            k1[j] = p.rs[j] * m.x;
+            k2[j] = p.rs[j] * (p.rs[j] * m.y);
+        });
         for (int64_t r = w.first + thread; r < w.end; r += kGnAhead * threads) {
             GnRaw<T, V, SAVED> raw[kGnAhead];
             GnRaw<T, V, false> grad[kGnAhead];
@@ -495,15 +607,13 @@ __global__ __launch_bounds__(kBlock) void k_gn_dx(GnShape s, bool keep, const fl
 #pragma unroll
             for (int u = 0; u < kGnAhead; ++u) {
                 if (u >= rows) break;
-                float f[V], g[V], h;
-                raw[u].widen(k, f);
+                float d[V], g[V];
+                raw[u].center(k, p.mu, d);
                 grad[u].widen(k, g);
+                gn_dz<T, V, ACT>(g, d, zw, p, raw[u], grad[u], k);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float dz = dz_of<ACT>(g[j], f[j], p.mu[j], p.rs[j], p.w[j], p.b[j], h);
-                    f[j] = p.rs[j] * (__fmaf_rn(dz, p.w[j], -m[j].x) - h * m[j].y);
-                }
-                gn_store<T, V>(keep, to + (r + u * threads) * dx.row, k, f);
+                for (int j = 0; j < V; ++j) d[j] = __fmaf_rn(g[j], zw[j], -__fmaf_rn(d[j], k2[j], k1[j]));
+                gn_store<T, V>(keep, to + (r + u * threads) * dx.row, k, d);
             }
         }
     }
