@@ -14,8 +14,11 @@ using namespace liec;
 
 namespace {
 
-// Results of up to the memory-side cache's 256 MB are left there for the operation that reads them next.
-bool keeps(int64_t bytes) { return bytes <= (int64_t)256 << 20; }
+// Results are left in the memory-side cache of 256 MB for the operation that reads them next if what was read for them fits beside them;
+// larger ones are streamed past it, so that a normalisation's second pass finds in it what the first one read and the next
+// call's first pass does not wait for results to leave it (stats and apply of 128 images of 56 x 56 x 256 bf16, 206 MB: 41 + 79 against 55 + 76 us,
+// of 268 MB 47 + 92 against 75 + 92).
+bool keeps(int64_t bytes) { return bytes <= (int64_t)128 << 20; }
 
 // Blocks of a launch whose blocks walk over the work: far more than are resident, and within what a launch may have.
 uint32_t grid_of(int64_t works) { return (uint32_t)std::max<int64_t>(1, std::min<int64_t>(works, (int64_t)1 << 22)); }
@@ -117,7 +120,10 @@ bool valid_norm(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
     return (double)N * (double)B * (double)std::max<int64_t>(S, 1) * (double)C <= (double)kMostValues;
 }
 
-constexpr int64_t kGnBlocks = 2048;    // that a launch should have at least, where there is work for them
+// Blocks that a launch should have at least, where there is work for them: of sums, whose number sets how many partial sums a group has
+// (4 x 4 images of 128 x 128 x 512 bf16: 512 blocks 70 + 9 us, 1024 75 + 15, 2048 78 + 26), and of what is written from them (512 blocks
+// 116 us, 1024 92, 2048 91, 8192 88).
+constexpr int64_t kGnSumBlocks = 512, kGnBlocks = 2048;
 constexpr int64_t kGnChain = 256;      // positions that a thread adds up
 
 int log_of(int64_t n) {                // of the next power of two
@@ -126,7 +132,7 @@ int log_of(int64_t n) {                // of the next power of two
     return r;
 }
 
-GnShape shape_of(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
+GnShape shape_of(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G, int64_t blocks = kGnSumBlocks) {
     GnShape s{};
     const int64_t pieces = C < 8 ? C : ceil_div(C, 8);
     s.images = N * B, s.B = B, s.S = S, s.C = (uint32_t)C, s.G = (uint32_t)G, s.per_group = (uint32_t)(C / G), s.whole = C / G % 8 == 0;
@@ -134,7 +140,7 @@ GnShape shape_of(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
     s.lanes_log = (uint32_t)std::min(6, C < 8 ? log_of(C) : std::max(2, log_of(pieces)));
     s.tiles = (uint32_t)ceil_div(pieces, (int64_t)1 << s.lanes_log);
     const int64_t threads = kBlock >> s.lanes_log;
-    const int64_t want = ceil_div(kGnBlocks, std::max<int64_t>(1, s.images * s.tiles));
+    const int64_t want = ceil_div(blocks, std::max<int64_t>(1, s.images * s.tiles));
     s.per = std::max(ceil_div(S, want), std::min(S, kGnAhead * threads));
     s.per = std::max<int64_t>(1, std::min(s.per, kGnChain * threads));
     s.splits = (uint32_t)std::max<int64_t>(1, ceil_div(S, s.per));
@@ -145,13 +151,13 @@ uint32_t gn_group_blocks(const GnShape& s) { return grid_of(ceil_div(s.images * 
 int64_t gn_partials(const GnShape& s) { return s.images * s.splits * 2 * (int64_t)s.C; }
 GnImages images_of(const liec_images* x) { return x && x->data ? GnImages{x->data, x->worker_stride, x->image_stride, x->row_stride} : GnImages{nullptr, 0, 0, 0}; }
 
-// Does a block hold a group's positions, `most` of them per thread?  Spans of `wide` bytes per position if they fit, then half and a
-// quarter of that, in multiples of `least` channels (those that share an exponent of a checkpoint, or a vector); rows whose groups do
-// not come to that are taken whole.
-bool hold(const GnShape& s, int64_t size, int64_t most, int64_t least, GnHeld* h) {
+// Does a block of up to `threads` threads hold a group's positions, `most` of them per thread?  Spans of 128 bytes per position if they
+// fit, then narrower ones down to `narrow`, in multiples of `least` channels (those that share an exponent of a checkpoint, or a
+// vector); rows whose groups do not come to that are taken whole.
+bool hold(const GnShape& s, int64_t size, int64_t most, int64_t threads, int64_t least, int64_t narrow, GnHeld* h) {
     const int64_t pg = s.per_group, C = s.C;
-    if (C < 8 || s.S > most * kGnHeldMost) return false;
-    for (int64_t wide = 128; wide >= 32; wide /= 2) {
+    if (C < 8 || s.S > most * threads) return false;
+    for (int64_t wide = 128; wide >= narrow; wide /= 2) {
         int64_t groups = ceil_div(wide / size, pg);
         while (groups < s.G && groups * pg % least) ++groups;
         h->span = (uint32_t)std::min(groups * pg, C);
@@ -160,7 +166,7 @@ bool hold(const GnShape& s, int64_t size, int64_t most, int64_t least, GnHeld* h
         if (h->lanes_log > 6) continue;
         h->rows_log = (uint32_t)log_of(ceil_div(s.S, most));
         while (h->lanes_log + h->rows_log < 8 && ((int64_t)1 << h->rows_log) < s.S) ++h->rows_log;
-        if (((int64_t)1 << (h->lanes_log + h->rows_log)) > kGnHeldMost) continue;
+        if (((int64_t)1 << (h->lanes_log + h->rows_log)) > threads) continue;
         // more images where one is small: of one worker, so as many as its number of them is a multiple of
         h->images_log = 0;
         while (h->lanes_log + h->rows_log + h->images_log < 8 && s.B % ((int64_t)2 << h->images_log) == 0) ++h->images_log;
@@ -185,7 +191,7 @@ int64_t held_bytes(const GnShape& s, const GnHeld& h, bool backward) {
 uint32_t held_grid(const GnShape& s, const GnHeld& h) { return grid_of((s.images >> h.images_log) * h.spans); }
 
 struct GnForward {
-    GnShape s;
+    GnShape s, each;                   // of sums, and of what is written from them
     GnImages x, y;
     LnParam w, b;
     float *mean, *rstd, *partial, eps;
@@ -212,20 +218,27 @@ void gn_forward_of(const GnForward& a) {
     k_gn_groups<0><<<gn_group_blocks(a.s), kBlock, 0, a.st>>>(a.s, a.partial, a.eps, a.mean, a.rstd);
     const auto apply = a.saved.q ? (a.act == kActNone ? k_gn_apply<T, V, kActNone, true> : a.act == kActRelu ? k_gn_apply<T, V, kActRelu, true> : k_gn_apply<T, V, kActSilu, true>)
                                  : (a.act == kActNone ? k_gn_apply<T, V, kActNone, false> : a.act == kActRelu ? k_gn_apply<T, V, kActRelu, false> : k_gn_apply<T, V, kActSilu, false>);
-    apply<<<grid, kBlock, 0, a.st>>>(a.s, a.keep, a.mean, a.rstd, a.x, a.y, a.w, a.b, a.saved);
+    apply<<<grid_of(gn_works_of(a.each)), kBlock, 0, a.st>>>(a.each, a.keep, a.mean, a.rstd, a.x, a.y, a.w, a.b, a.saved);
 }
-// Positions of a thread in registers: 128 of those for values.
+// Images that blocks hold.  Positions of a thread: 32 registers for values (four times as many leave two waves to a SIMD, whose loads and
+// arithmetic do not overlap: 128 images of 56 x 56 x 256 bf16 116 to 125 us against 124 in two passes, of 28 x 28 x 512 with a checkpoint
+// 75 against 51).  Blocks of 512 threads, two to a compute unit, before larger ones: 128 images of 28 x 28 x 512 bf16 51.8 us, with
+// 1024 threads and wider spans 53.7, in two passes 71.1; fp32 with 1024 threads 113, in two passes 145.
+template <typename T>
+bool held_forward(const GnForward& a, GnHeld* h) {
+    constexpr int most = sizeof(T) == 2 ? 8 : 4;
+    if (!hold(a.s, sizeof(T), most, 512, kSavedCols, 32, h) && !hold(a.s, sizeof(T), most, kGnHeldMost, kSavedCols, 32, h)) return false;
+    return held_bytes(a.s, *h, false) <= kGnHeldBytes && near(a.x, a.s, *h, sizeof(T)) && near(a.y, a.s, *h, sizeof(T));
+}
 template <typename T>
 void gn_forward_of(const GnForward& a) {
-    constexpr int most = sizeof(T) == 2 ? 32 : 16;
     GnHeld h;
-    if (hold(a.s, sizeof(T), most, kSavedCols, &h) && held_bytes(a.s, h, false) <= kGnHeldBytes && near(a.x, a.s, h, sizeof(T)) && near(a.y, a.s, h, sizeof(T)))
-        h.rows <= most / 4 ? gn_held_of<T, most / 4>(a, h) : gn_held_of<T, most>(a, h);
+    if (held_forward<T>(a, &h)) gn_held_of<T, sizeof(T) == 2 ? 8 : 4>(a, h);
     else a.s.C < 8 ? gn_forward_of<T, 1>(a) : gn_forward_of<T, 8>(a);
 }
 
 struct GnBackward {
-    GnShape s;
+    GnShape s, each;
     GnImages dy, x, dx;
     Saved saved;
     LnParam w, b, dw, db;
@@ -254,7 +267,7 @@ void gn_backward_of(const GnBackward& a) {
     if (!a.dx.data) return;
     float2* const means = reinterpret_cast<float2*>(a.partial + gn_partials(a.s));
     k_gn_means<0><<<gn_group_blocks(a.s), kBlock, 0, a.st>>>(a.s, a.partial, a.w, means);
-    k_gn_dx<T, V, ACT, SAVED><<<grid, kBlock, 0, a.st>>>(a.s, a.keep, a.mean, a.rstd, means, a.dy, a.x, a.saved, a.dx, a.w, a.b);
+    k_gn_dx<T, V, ACT, SAVED><<<grid_of(gn_works_of(a.each)), kBlock, 0, a.st>>>(a.each, a.keep, a.mean, a.rstd, means, a.dy, a.x, a.saved, a.dx, a.w, a.b);
 }
 template <typename T, int V, int ACT>
 void gn_backward_of(const GnBackward& a) { a.saved.q ? gn_backward_of<T, V, ACT, true>(a) : gn_backward_of<T, V, ACT, false>(a); }
@@ -262,14 +275,20 @@ template <typename T, int V>
 void gn_backward_of(const GnBackward& a, int act) {
     act == kActNone ? gn_backward_of<T, V, kActNone>(a) : act == kActRelu ? gn_backward_of<T, V, kActRelu>(a) : gn_backward_of<T, V, kActSilu>(a);
 }
+// Half as many positions, for two operands, and spans of 64 bytes at least: 128 images of 28 x 28 x 512 bf16 in spans of 32 bytes 129 us, in
+// two passes 100; of 14 x 14 x 1024 fp32, held, 95 against 114.
+template <typename T>
+bool held_backward(const GnBackward& a, GnHeld* h) {
+    if (!hold(a.s, sizeof(T), sizeof(T) == 2 ? 4 : 2, 512, 8, 64, h) || held_bytes(a.s, *h, true) > kGnHeldBytes) return false;
+    const GnImages rows{nullptr, 0, a.s.S * (int64_t)a.s.C, a.s.C};      // of a checkpoint
+    return near(a.x, a.s, *h, sizeof(T)) && near(a.dy, a.s, *h, sizeof(T)) && near(a.dx, a.s, *h, sizeof(T)) && near(rows, a.s, *h, 1);
+}
 // Returns the number of partial sums of all images.
 template <typename T>
 int64_t gn_backward_of(const GnBackward& a, int act) {
-    constexpr int most = sizeof(T) == 2 ? 16 : 8;
     GnHeld h;
-    if (hold(a.s, sizeof(T), most, 8, &h) && held_bytes(a.s, h, true) <= kGnHeldBytes && near(a.x, a.s, h, sizeof(T)) && near(a.dy, a.s, h, sizeof(T)) &&
-        near(a.dx, a.s, h, sizeof(T)) && near(GnImages{nullptr, 0, a.s.S * (int64_t)a.s.C, a.s.C}, a.s, h, 1)) {
-        h.rows <= most / 4 ? gn_held_of<T, most / 4>(a, h, act) : gn_held_of<T, most>(a, h, act);
+    if (held_backward<T>(a, &h)) {
+        gn_held_of<T, sizeof(T) == 2 ? 4 : 2>(a, h, act);
         return a.s.images >> h.images_log;
     }
     a.s.C < 8 ? gn_backward_of<T, 1>(a, act) : gn_backward_of<T, 8>(a, act);
@@ -386,7 +405,7 @@ liec_status liec_group_norm(const liec_images* x, const liec_param* weight, cons
         for (const Span& v : written)
             if (&v < &w && spans_meet(v, w)) return LIEC_EINVAL;
     }
-    const GnForward a{shape_of(N, B, S, C, G), images_of(x), images_of(y), param_of(weight, param_dtype), param_of(bias, param_dtype), mean, rstd,
+    const GnForward a{shape_of(N, B, S, C, G), shape_of(N, B, S, C, G, kGnBlocks), images_of(x), images_of(y), param_of(weight, param_dtype), param_of(bias, param_dtype), mean, rstd,
                       static_cast<float*>(workspace), eps, saved_of(saved), keeps((int64_t)N * B * S * C * size), activation, (hipStream_t)hip_stream};
     if (dtype == LIEC_F32) gn_forward_of<float>(a);
     else if (dtype == LIEC_BF16) gn_forward_of<bf16>(a);
@@ -442,7 +461,7 @@ liec_status liec_group_norm_backward(const liec_images* dy, const liec_images* x
         }
     }
     const hipStream_t st = (hipStream_t)hip_stream;
-    GnBackward a{shape_of(N, B, S, C, G), images_of(dy), images_of(x), images_of(dx), saved_of(saved), param_of(weight, param_dtype), param_of(bias, param_dtype),
+    GnBackward a{shape_of(N, B, S, C, G), shape_of(N, B, S, C, G, kGnBlocks), images_of(dy), images_of(x), images_of(dx), saved_of(saved), param_of(weight, param_dtype), param_of(bias, param_dtype),
                  param_of(dweight, param_dtype), param_of(dbias, param_dtype), mean, rstd, static_cast<float*>(workspace),
                  keeps((int64_t)N * B * S * C * size), st};
     int64_t parts = 0;

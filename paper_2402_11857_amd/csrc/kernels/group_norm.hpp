@@ -12,6 +12,8 @@
 // 16 bytes wide.  The last 8 channels of a row whose length is no multiple of 8 start 8 before its end; what they share with
 // the ones before is left out where it is stored.
 #pragma once
+#include <type_traits>
+
 #include "checkpoint.hpp"
 
 namespace liec {
@@ -174,6 +176,15 @@ __device__ __forceinline__ GnWork gn_work(const GnShape& s, int64_t work) {
 }
 
 constexpr int kGnAhead = 4;            // positions of a thread requested together
+
+// A thread's positions of a strip: f(first of them, how many: kGnAhead, as a constant, or one at a time for what is left), with the
+// distance between them.
+template <typename F>
+__device__ __forceinline__ void gn_walk(const GnWork& w, uint32_t thread, uint32_t threads, F f) {
+    int64_t r = w.first + thread;
+    for (; r + (kGnAhead - 1) * (int64_t)threads < w.end; r += kGnAhead * threads) f(r, std::integral_constant<int, kGnAhead>{});
+    for (; r < w.end; r += threads) f(r, std::integral_constant<int, 1>{});
+}
 constexpr int kGnTile = 512;           // channels of a tile, at most
 
 // Stores a block's sums per channel, lds[wave][channel of the tile] of `waves` waves put together by `join`.
@@ -199,8 +210,8 @@ __device__ __forceinline__ void gn_join(float n, float& mean, float& squares, fl
 }
 
 // Mean and squares around it of each channel over a strip of an image's positions.  A thread takes its values around the mean p of its
-// first four: with n of them (at most 256) and m their mean, (p - m)^2 <= n / 4 of their variance, so that taking n (p - m)^2 off
-// again costs at most 64 u of it per addition's u.
+// first four (or, of less than four in all, its first): with n of them (at most 256) and m their mean, (p - m)^2 <= n / 4 of
+// their variance, so that taking n (p - m)^2 off again costs at most 64 u of it per addition's u.
 template <typename T, int V>
 __global__ __launch_bounds__(kBlock) void k_gn_stats(GnShape s, GnImages x, float* __restrict__ partial) {
     __shared__ float lds_mean[kBlock / 64][kGnTile], lds_squares[kBlock / 64][kGnTile], lds_n[kBlock / 64];
@@ -212,34 +223,36 @@ __global__ __launch_bounds__(kBlock) void k_gn_stats(GnShape s, GnImages x, floa
         float p[V], sum[V], squares[V], n = 0.f;
 #pragma unroll
         for (int j = 0; j < V; ++j) p[j] = sum[j] = squares[j] = 0.f;
-        for (int64_t r = w.first + thread; k.any && r < w.end; r += kGnAhead * threads) {
-            GnRaw<T, V, false> raw[kGnAhead];
-            const uint32_t rows = (uint32_t)min((int64_t)kGnAhead, (w.end - r + threads - 1) / threads);
+        const int64_t step = threads * x.row;
+        if (k.any)
+            gn_walk(w, thread, threads, [&](int64_t r, auto rows) {
+                constexpr int R = decltype(rows)::value;
+                GnRaw<T, V, false> raw[R];
+                const T* const first = at + r * x.row;
 #pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) raw[u].load(at + (u < (int)rows ? r + u * threads : r) * x.row, k);
-            float f[kGnAhead][V];
+                for (int u = 0; u < R; ++u) raw[u].load(first + u * step, k);
+                float f[R][V];
 #pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) raw[u].widen(k, f[u]);
-            if (n == 0.f) {
+                for (int u = 0; u < R; ++u) raw[u].widen(k, f[u]);
+                if (n == 0.f) {
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float t = f[0][j];
-                    for (int u = 1; u < kGnAhead; ++u) t += u < (int)rows ? f[u][j] : 0.f;
-                    p[j] = t / (float)rows;
+                    for (int j = 0; j < V; ++j) {
+                        p[j] = f[0][j];
+#pragma unroll
+                        for (int u = 1; u < R; ++u) p[j] += f[u][j];
+                        p[j] *= 1.f / R;
+                    }
                 }
-            }
 #pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                if (u >= (int)rows) break;
+                for (int u = 0; u < R; ++u)
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float d = f[u][j] - p[j];
-                    sum[j] += d;
-                    squares[j] = __fmaf_rn(d, d, squares[j]);
-                }
-            }
-            n += (float)rows;
-        }
+                    for (int j = 0; j < V; ++j) {
+                        const float d = f[u][j] - p[j];
+                        sum[j] += d;
+                        squares[j] = __fmaf_rn(d, d, squares[j]);
+                    }
+                n += (float)R;
+            });
 #pragma unroll
         for (int j = 0; j < V; ++j) {
             const float d = n > 0.f ? sum[j] / n : 0.f;
@@ -281,6 +294,7 @@ __device__ __forceinline__ void gn_each_part(const GnShape& s, int64_t group, F 
     const int64_t image = group / s.G;
     const uint32_t first = (uint32_t)(group - image * s.G) * s.per_group, lane = threadIdx.x & 63;
     const uint32_t wide_log = s.per_group >= 64 ? 6 : 32 - __clz((int)s.per_group), wide = 1u << wide_log;
+#pragma unroll 4
     for (uint32_t split = lane >> wide_log; split < s.splits; split += 64 >> wide_log)
         for (uint32_t c = lane & (wide - 1); c < s.per_group; c += wide) f((size_t)(image * s.splits + split) * 2 * s.C + first + c, first + c, split);
 }
@@ -418,25 +432,27 @@ __global__ __launch_bounds__(kBlock) void k_gn_apply(GnShape s, bool keep, const
         p.load(s, w.image, k, mean, rstd, weight, bias);
 #pragma unroll
         for (int j = 0; j < V; ++j) p.rs[j] *= p.w[j];
-        for (int64_t r = w.first + thread; r < w.end; r += kGnAhead * threads) {
-            GnRaw<T, V, false> raw[kGnAhead];
-            const int rows = (int)min((int64_t)kGnAhead, (w.end - r + threads - 1) / threads);
+        const int64_t x_step = threads * x.row, y_step = threads * y.row;
+        gn_walk(w, thread, threads, [&](int64_t r, auto rows) {
+            constexpr int R = decltype(rows)::value;
+            GnRaw<T, V, false> raw[R];
+            const T* const first = from + r * x.row;
+            T* const out_first = to + r * y.row;
             if (k.any) {
 #pragma unroll
-                for (int u = 0; u < kGnAhead; ++u) raw[u].load(from + (u < rows ? r + u * threads : r) * x.row, k);
+                for (int u = 0; u < R; ++u) raw[u].load(first + u * x_step, k);
             }
 #pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                if (u >= rows) break;
+            for (int u = 0; u < R; ++u) {
                 float f[V];
                 if (k.any) raw[u].widen(k, f);
                 if (SAVE) gn_save<V>(out, w.image * s.S + r + u * threads, s, k, f);
                 if (!k.any) continue;
 #pragma unroll
                 for (int j = 0; j < V; ++j) f[j] = act_of<T, ACT>(__fmaf_rn(f[j] - p.mu[j], p.rs[j], p.b[j]));
-                gn_store<T, V>(keep, to + (r + u * threads) * y.row, k, f);
+                gn_store<T, V>(keep, out_first + u * y_step, k, f);
             }
-        }
+        });
     }
 }
 
@@ -475,11 +491,19 @@ __device__ __forceinline__ void gn_dz(float (&g)[V], const float (&d)[V], const 
     if (ACT == kActRelu && __builtin_expect(near, 0)) gn_dz_exact<V>(g, p, raw, grad, k);
 }
 
-template <typename T, int V, bool SAVED>
-__device__ __forceinline__ void gn_load(GnRaw<T, V, SAVED>& raw, const T* image, const GnImages& x, const Saved& saved, const GnShape& s, const GnWork& w, int64_t r,
-                                        const GnColumns& k) {
-    if constexpr (SAVED) raw.load(saved, w.image * s.S + r, s.C, (s.C + kSavedCols - 1) / kSavedCols, k);
-    else raw.load(image + r * x.row, k);
+// R positions of x, or its checkpoint, and dy.
+template <typename T, int V, bool SAVED, int R>
+__device__ __forceinline__ void gn_load(GnRaw<T, V, SAVED> (&raw)[R], GnRaw<T, V, false> (&grad)[R], const T* xs, const GnImages& x, const Saved& saved, const T* gs,
+                                        const GnImages& dy, const GnShape& s, const GnWork& w, int64_t r, uint32_t threads, const GnColumns& k) {
+    const int64_t x_step = threads * x.row, g_step = threads * dy.row;
+    const T* const x_first = xs + r * x.row;
+    const T* const g_first = gs + r * dy.row;
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+        if constexpr (SAVED) raw[u].load(saved, w.image * s.S + r + u * threads, s.C, (s.C + kSavedCols - 1) / kSavedCols, k);
+        else raw[u].load(x_first + u * x_step, k);
+        grad[u].load(g_first + u * g_step, k);
+    }
 }
 
 // Sums of dz h and of dz over a strip of an image's positions.
@@ -501,30 +525,25 @@ __global__ __launch_bounds__(kBlock) void k_gn_sums(GnShape s, const float* __re
         float sum_h[V], sum_1[V];
 #pragma unroll
         for (int j = 0; j < V; ++j) sum_h[j] = sum_1[j] = 0.f;
-        for (int64_t r = w.first + thread; k.any && r < w.end; r += kGnAhead * threads) {
-            GnRaw<T, V, SAVED> raw[kGnAhead];
-            GnRaw<T, V, false> grad[kGnAhead];
-            const int rows = (int)min((int64_t)kGnAhead, (w.end - r + threads - 1) / threads);
+        if (k.any)
+            gn_walk(w, thread, threads, [&](int64_t r, auto rows) {
+                constexpr int R = decltype(rows)::value;
+                GnRaw<T, V, SAVED> raw[R];
+                GnRaw<T, V, false> grad[R];
+                gn_load<T, V, SAVED, R>(raw, grad, xs, x, saved, gs, dy, s, w, r, threads, k);
 #pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                const int64_t at = u < rows ? r + u * threads : r;
-                gn_load<T, V, SAVED>(raw[u], xs, x, saved, s, w, at, k);
-                grad[u].load(gs + at * dy.row, k);
-            }
+                for (int u = 0; u < R; ++u) {
+                    float d[V], g[V];
+                    raw[u].center(k, p.mu, d);
+                    grad[u].widen(k, g);
+                    gn_dz<T, V, ACT>(g, d, zw, p, raw[u], grad[u], k);
 #pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                if (u >= rows) break;
-                float d[V], g[V];
-                raw[u].center(k, p.mu, d);
-                grad[u].widen(k, g);
-                gn_dz<T, V, ACT>(g, d, zw, p, raw[u], grad[u], k);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    sum_1[j] += g[j];
-                    sum_h[j] = __fmaf_rn(g[j], d[j], sum_h[j]);
+                    for (int j = 0; j < V; ++j) {
+                        sum_1[j] += g[j];
+                        sum_h[j] = __fmaf_rn(g[j], d[j], sum_h[j]);
+                    }
                 }
-            }
-        }
+            });
 #pragma unroll
         for (int j = 0; j < V; ++j) sum_h[j] *= p.rs[j];
         for (uint32_t off = 1u << s.lanes_log; off < 64; off <<= 1) {
@@ -594,28 +613,24 @@ __global__ __launch_bounds__(kBlock) void k_gn_dx(GnShape s, bool keep, const fl
             k1[j] = p.rs[j] * m.x;
             k2[j] = p.rs[j] * (p.rs[j] * m.y);
         });
-        for (int64_t r = w.first + thread; r < w.end; r += kGnAhead * threads) {
-            GnRaw<T, V, SAVED> raw[kGnAhead];
-            GnRaw<T, V, false> grad[kGnAhead];
-            const int rows = (int)min((int64_t)kGnAhead, (w.end - r + threads - 1) / threads);
+        const int64_t step = threads * dx.row;
+        gn_walk(w, thread, threads, [&](int64_t r, auto rows) {
+            constexpr int R = decltype(rows)::value;
+            GnRaw<T, V, SAVED> raw[R];
+            GnRaw<T, V, false> grad[R];
+            gn_load<T, V, SAVED, R>(raw, grad, xs, x, saved, gs, dy, s, w, r, threads, k);
+            T* const first = to + r * dx.row;
 #pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                const int64_t at = u < rows ? r + u * threads : r;
-                gn_load<T, V, SAVED>(raw[u], xs, x, saved, s, w, at, k);
-                grad[u].load(gs + at * dy.row, k);
-            }
-#pragma unroll
-            for (int u = 0; u < kGnAhead; ++u) {
-                if (u >= rows) break;
+            for (int u = 0; u < R; ++u) {
                 float d[V], g[V];
                 raw[u].center(k, p.mu, d);
                 grad[u].widen(k, g);
                 gn_dz<T, V, ACT>(g, d, zw, p, raw[u], grad[u], k);
 #pragma unroll
                 for (int j = 0; j < V; ++j) d[j] = __fmaf_rn(g[j], zw[j], -__fmaf_rn(d[j], k2[j], k1[j]));
-                gn_store<T, V>(keep, to + (r + u * threads) * dx.row, k, d);
+                gn_store<T, V>(keep, first + u * step, k, d);
             }
-        }
+        });
     }
 }
 

@@ -16,7 +16,7 @@
 
 namespace liec {
 
-constexpr int kGnHeldMost = 512;       // threads, with 256 registers each
+constexpr int kGnHeldMost = 1024;      // threads
 
 struct GnHeld {
     uint32_t span, spans;              // channels of a block, blocks of an image
@@ -116,21 +116,25 @@ __device__ __forceinline__ float gn_wave_total(float v) {
     for (uint32_t bit = 0; bit < 6; ++bit) v = gn_rows_sum(v, bit, bit + 1);
     return v;
 }
-// A wave for each group of each image: f(number of the group, sums of its entries in `a` and `b`).
+// For each group of each image: f(number of the group, sums of its entries in `a` and `b`).  A thread to a group where it has few entries,
+// a wave otherwise.
 template <bool TWO, typename F>
 __device__ __forceinline__ void gn_groups_total(const GnShape& s, const GnHeld& h, const GnPlace& p, uint32_t entries, uint32_t waves, uint32_t group, const float* a,
                                                 const float* b, F f) {
-    const uint32_t groups = p.channels / s.per_group, many = groups << h.images_log, lane = threadIdx.x & 63;
-    for (uint32_t q = threadIdx.x >> 6; q < many; q += blockDim.x >> 6) {
+    const uint32_t groups = p.channels / s.per_group, many = groups << h.images_log, lane = threadIdx.x & 63, each = group * waves;
+    const bool few = each <= 16;
+    for (uint32_t q = few ? threadIdx.x : threadIdx.x >> 6; q < many; q += few ? blockDim.x : blockDim.x >> 6) {
         const uint32_t im = q / groups, g = q - im * groups, at = (im * entries + g * group) * waves;
         float va = 0.f, vb = 0.f;
-        for (uint32_t i = lane; i < group * waves; i += 64) {
+        for (uint32_t i = few ? 0 : lane; i < each; i += few ? 1 : 64) {
             va += a[at + i];
             if (TWO) vb += b[at + i];
         }
-        va = gn_wave_total(va);
-        if (TWO) vb = gn_wave_total(vb);
-        if (lane == 0) f(q, va, vb);
+        if (!few) {
+            va = gn_wave_total(va);
+            if (TWO) vb = gn_wave_total(vb);
+        }
+        if (few || lane == 0) f(q, va, vb);
     }
 }
 
