@@ -131,7 +131,9 @@ def run_both(x, dy, G, w, b, act, eps=EPS):
 SHAPES = [((1, 1, 1, 1), 1), ((2, 1, 1, 4), 2), ((3, 2, 5, 7), 7), ((1, 3, 9, 8), 1), ((2, 2, 4, 9), 3), ((2, 3, 17, 24), 3), ((1, 2, 64, 30), 3), ((3, 2, 33, 33), 11),
           ((2, 2, 49, 64), 8), ((5, 3, 27 * 31, 90), 9), ((1, 1, 3000, 8), 2), ((1, 2, 700, 256), 32), ((2, 1, 130, 513), 1), ((1, 2, 50, 1030), 5), ((2, 1, 7, 4096), 64),
           ((1, 1, 1, 2048), 16), ((2, 40, 1, 96), 4), ((1, 300, 4, 32), 8), ((1, 1, 70_001, 3), 1), ((1, 1, 20_003, 40), 5), ((2, 2, 1025, 128), 1), ((1, 2, 2049, 16), 16),
-          ((1, 1, 5000, 520), 8), ((1, 1, 257, 4097), 17), ((3, 1, 300, 65), 65)]
+          ((1, 1, 5000, 520), 8), ((1, 1, 257, 4097), 17), ((3, 1, 300, 65), 65),
+          ((2, 2, 30, 512), 1), ((1, 3, 20, 1024), 2), ((2, 4, 3, 416), 1), ((3, 6, 9, 72), 1), ((2, 3, 100, 44), 11), ((1, 2, 700, 44), 11), ((4, 16, 1, 1000), 8),
+          ((2, 2, 513, 200), 25), ((2, 32, 2, 40), 5), ((1, 64, 1, 16), 1), ((2, 5, 1, 8), 8), ((1, 2, 4096, 64), 2), ((1, 2, 4097, 64), 2), ((2, 2, 1023, 96), 3)]
 
 
 @pytest.mark.parametrize("shape,G", SHAPES)
