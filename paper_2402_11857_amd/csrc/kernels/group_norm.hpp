@@ -11,6 +11,11 @@
 // around it go together in the group's.  So a thread keeps 8 channels and walks positions, whatever the groups' width, and loads are
 // 16 bytes wide.  The last 8 channels of a row whose length is no multiple of 8 start 8 before its end; what they share with
 // the ones before is left out where it is stored.
+//
+// These are the kernels for images that no block holds: two passes over them, bound by memory and, with an activation, by arithmetic
+// beside it.  16 x 8 images of 56 x 56 x 256 bf16, ReLU: forward 36 us for the sums (5.7 TB/s), 5 for the groups, 78 for y
+// (5.2 TB/s of x and y); backward from a checkpoint 63 for the sums (4.9 TB/s), 5 + 5 for what comes of them, 96 for dx (5.4
+// TB/s). 
 #pragma once
 #include <type_traits>
 
