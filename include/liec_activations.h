@@ -63,7 +63,8 @@ typedef struct {
     int64_t worker_stride, image_stride, row_stride;
 } liec_images;
 
-/* Bytes of scratch that liec_group_norm and liec_group_norm_backward need; -1 for bad arguments.  Host only. */
+/* Bytes of scratch that liec_group_norm and liec_group_norm_backward need, 16 per channel and at most 256 MB more (or what one image's
+ * sums take, if that is more: many images go in parts); -1 for bad arguments.  Host only. */
 int64_t liec_group_norm_workspace(int32_t N, int64_t B, int64_t S, int64_t C, int64_t G);
 
 /*

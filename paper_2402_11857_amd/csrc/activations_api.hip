@@ -190,7 +190,44 @@ int64_t held_bytes(const GnShape& s, const GnHeld& h, bool backward) {
 }
 uint32_t held_grid(const GnShape& s, const GnHeld& h) { return grid_of((s.images >> h.images_log) * h.spans); }
 
+// Images whose partial sums are in the scratch at a time: all of them, whole workers, or some of one worker's.  Many images of few
+// positions would take more scratch than they take themselves, 8 bytes per image and channel.
+constexpr int64_t kGnScratch = (int64_t)256 << 20;
+struct GnChunk {
+    int64_t workers, images;
+};
+int64_t gn_scratch(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
+    const GnShape s = shape_of(N, B, S, C, G);
+    return ceil_div(gn_partials(s) * (int64_t)sizeof(float) + s.images * G * (int64_t)sizeof(float2), 16) * 16;
+}
+GnChunk gn_chunk(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
+    const int64_t most = std::max<int64_t>(1, kGnScratch / (shape_of(N, B, S, C, G).splits * 8 * C + 8 * G));
+    return N * B <= most ? GnChunk{N, B} : B <= most ? GnChunk{most / B, B} : GnChunk{1, most};
+}
+// Of the chunks, the last ones among them, whose strips may be shorter.
+int64_t gn_chunk_scratch(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
+    const GnChunk c = gn_chunk(N, B, S, C, G);
+    int64_t need = gn_scratch(c.workers, c.images, S, C, G);
+    if (N % c.workers) need = std::max(need, gn_scratch(N % c.workers, c.images, S, C, G));
+    if (B % c.images) need = std::max(need, gn_scratch(c.workers, B % c.images, S, C, G));
+    return need;
+}
+int64_t gn_run_bytes(int64_t C) { return 2 * C * (int64_t)sizeof(double); }   // weight gradients that chunks add to
+
+GnImages from(const GnImages& x, int64_t worker, int64_t image, int64_t size) {
+    GnImages r = x;
+    if (r.data) r.data = static_cast<char*>(r.data) + (worker * x.worker + image * x.image) * size;
+    return r;
+}
+LnParam from(const LnParam& p, int64_t worker) {
+    LnParam r = p;
+    if (r.data) r.data = static_cast<char*>(r.data) + worker * p.stride * size_of((int)p.type);
+    return r;
+}
+Saved from(const Saved& s, int64_t rows, int64_t C) { return s.q ? Saved{s.q + rows * C, s.e + rows * groups_of(C)} : s; }
+
 struct GnForward {
+    int64_t N;
     GnShape s, each;                   // of sums, and of what is written from them
     GnImages x, y;
     LnParam w, b;
@@ -233,20 +270,49 @@ bool held_forward(const GnForward& a, GnHeld* h) {
 template <typename T>
 void gn_forward_of(const GnForward& a) {
     GnHeld h;
-    if (held_forward<T>(a, &h)) gn_held_of<T, sizeof(T) == 2 ? 8 : 4>(a, h);
-    else a.s.C < 8 ? gn_forward_of<T, 1>(a) : gn_forward_of<T, 8>(a);
+    if (held_forward<T>(a, &h)) {
+        gn_held_of<T, sizeof(T) == 2 ? 8 : 4>(a, h);
+        return;
+    }
+    const int64_t B = a.s.B, S = a.s.S, C = a.s.C, G = a.s.G;
+    const GnChunk chunk = gn_chunk(a.N, B, S, C, G);
+    for (int64_t w = 0; w < a.N; w += chunk.workers)
+        for (int64_t b = 0; b < B; b += chunk.images) {
+            const int64_t workers = std::min(chunk.workers, a.N - w), images = std::min(chunk.images, B - b), at = w * B + b;
+            GnForward part = a;
+            part.s = shape_of(workers, images, S, C, G);
+            part.each = shape_of(workers, images, S, C, G, kGnBlocks);
+            part.x = from(a.x, w, b, sizeof(T)), part.y = from(a.y, w, b, sizeof(T));
+            part.w = from(a.w, w), part.b = from(a.b, w);
+            part.mean += at * G, part.rstd += at * G;
+            part.saved = from(a.saved, at * S, C);
+            C < 8 ? gn_forward_of<T, 1>(part) : gn_forward_of<T, 8>(part);
+        }
 }
 
 struct GnBackward {
+    int64_t N;
     GnShape s, each;
     GnImages dy, x, dx;
     Saved saved;
     LnParam w, b, dw, db;
     const float *mean, *rstd;
+    double* run;
     float* partial;
+    int64_t scratch;                   // bytes behind `partial`
     bool keep;
     hipStream_t st;
 };
+
+// What comes of partial sums, `parts` of all workers: means for dx where there is one, and weight gradients, one sum for each worker or one over
+// all of them.
+void gn_after_sums(const GnBackward& a, int64_t parts, float2* means, bool first, bool last) {
+    const bool shared = a.N == 1 || (a.dw.data ? a.dw : a.db).stride == 0, params = a.dw.data || a.db.data;
+    const uint32_t blocks = means ? gn_group_blocks(a.s) : 0u, columns = (uint32_t)ceil_div(a.s.C, 32), workers = shared ? 1u : (uint32_t)a.N;
+    if (!blocks && !params) return;
+    const GnParamGrads p{shared ? parts : parts / a.N, workers, columns, a.run, first, last, a.dw, a.db};
+    k_gn_after_sums<0><<<blocks + (params ? grid_of(2 * (int64_t)columns * workers) : 0u), kBlock, 0, a.st>>>(a.s, blocks, a.partial, a.w, means, p);
+}
 
 template <typename T, int K, int ACT, bool SAVED>
 void gn_held_of(const GnBackward& a, const GnHeld& h) {
@@ -261,19 +327,21 @@ void gn_held_of(const GnBackward& a, const GnHeld& h, int act) {
 }
 
 template <typename T, int V, int ACT, bool SAVED>
-void gn_backward_of(const GnBackward& a) {
+void gn_backward_of(const GnBackward& a, bool first, bool last) {
     const uint32_t grid = grid_of(gn_works_of(a.s));
     k_gn_sums<T, V, ACT, SAVED><<<grid, kBlock, 0, a.st>>>(a.s, a.mean, a.rstd, a.dy, a.x, a.saved, a.w, a.b, a.partial);
-    if (!a.dx.data) return;
-    float2* const means = reinterpret_cast<float2*>(a.partial + gn_partials(a.s));
-    k_gn_means<0><<<gn_group_blocks(a.s), kBlock, 0, a.st>>>(a.s, a.partial, a.w, means);
-    k_gn_dx<T, V, ACT, SAVED><<<grid_of(gn_works_of(a.each)), kBlock, 0, a.st>>>(a.each, a.keep, a.mean, a.rstd, means, a.dy, a.x, a.saved, a.dx, a.w, a.b);
+    float2* const means = a.dx.data ? reinterpret_cast<float2*>(a.partial + gn_partials(a.s)) : nullptr;
+    gn_after_sums(a, a.s.images * a.s.splits, means, first, last);
+    if (means) k_gn_dx<T, V, ACT, SAVED><<<grid_of(gn_works_of(a.each)), kBlock, 0, a.st>>>(a.each, a.keep, a.mean, a.rstd, means, a.dy, a.x, a.saved, a.dx, a.w, a.b);
 }
 template <typename T, int V, int ACT>
-void gn_backward_of(const GnBackward& a) { a.saved.q ? gn_backward_of<T, V, ACT, true>(a) : gn_backward_of<T, V, ACT, false>(a); }
+void gn_backward_of(const GnBackward& a, bool first, bool last) {
+    a.saved.q ? gn_backward_of<T, V, ACT, true>(a, first, last) : gn_backward_of<T, V, ACT, false>(a, first, last);
+}
 template <typename T, int V>
-void gn_backward_of(const GnBackward& a, int act) {
-    act == kActNone ? gn_backward_of<T, V, kActNone>(a) : act == kActRelu ? gn_backward_of<T, V, kActRelu>(a) : gn_backward_of<T, V, kActSilu>(a);
+void gn_backward_of(const GnBackward& a, int act, bool first, bool last) {
+    const auto f = act == kActNone ? gn_backward_of<T, V, kActNone> : act == kActRelu ? gn_backward_of<T, V, kActRelu> : gn_backward_of<T, V, kActSilu>;
+    f(a, first, last);
 }
 // Half as many positions, for two operands, and spans of 64 bytes at least: 128 images of 28 x 28 x 512 bf16 in spans of 32 bytes 129 us, in
 // two passes 100; of 14 x 14 x 1024 fp32, held, 95 against 114.
@@ -283,16 +351,31 @@ bool held_backward(const GnBackward& a, GnHeld* h) {
     const GnImages rows{nullptr, 0, a.s.S * (int64_t)a.s.C, a.s.C};      // of a checkpoint
     return near(a.x, a.s, *h, sizeof(T)) && near(a.dy, a.s, *h, sizeof(T)) && near(a.dx, a.s, *h, sizeof(T)) && near(rows, a.s, *h, 1);
 }
-// Returns the number of partial sums of all images.
 template <typename T>
-int64_t gn_backward_of(const GnBackward& a, int act) {
+void gn_backward_of(const GnBackward& a, int act) {
+    const int64_t B = a.s.B, S = a.s.S, C = a.s.C, G = a.s.G;
     GnHeld h;
-    if (held_backward<T>(a, &h)) {
+    if (held_backward<T>(a, &h) && (a.s.images >> h.images_log) * 2 * C * (int64_t)sizeof(float) <= a.scratch) {
         gn_held_of<T, sizeof(T) == 2 ? 4 : 2>(a, h, act);
-        return a.s.images >> h.images_log;
+        return gn_after_sums(a, a.s.images >> h.images_log, nullptr, true, true);
     }
-    a.s.C < 8 ? gn_backward_of<T, 1>(a, act) : gn_backward_of<T, 8>(a, act);
-    return a.s.images * a.s.splits;
+    const GnChunk chunk = gn_chunk(a.N, B, S, C, G);
+    const bool over_all = (a.dw.data ? a.dw : a.db).stride == 0;
+    for (int64_t w = 0; w < a.N; w += chunk.workers)
+        for (int64_t b = 0; b < B; b += chunk.images) {
+            const int64_t at = w * B + b;
+            GnBackward part = a;
+            const int64_t images = std::min(chunk.images, B - b);
+            part.N = std::min(chunk.workers, a.N - w);
+            part.s = shape_of(part.N, images, S, C, G);
+            part.each = shape_of(part.N, images, S, C, G, kGnBlocks);
+            part.dy = from(a.dy, w, b, sizeof(T)), part.x = from(a.x, w, b, sizeof(T)), part.dx = from(a.dx, w, b, sizeof(T));
+            part.w = from(a.w, w), part.b = from(a.b, w), part.dw = from(a.dw, w), part.db = from(a.db, w);
+            part.mean += at * G, part.rstd += at * G;
+            part.saved = from(a.saved, at * S, C);
+            const bool first = b == 0 && (w == 0 || !over_all), last = b + images == B && (w + part.N == a.N || !over_all);
+            C < 8 ? gn_backward_of<T, 1>(part, act, first, last) : gn_backward_of<T, 8>(part, act, first, last);
+        }
 }
 
 bool valid_act(int a) { return a == LIEC_ACT_NONE || a == LIEC_ACT_RELU || a == LIEC_ACT_SILU; }
@@ -378,8 +461,7 @@ liec_status liec_checkpoint_load(const liec_checkpoint* saved, const liec_rows* 
 int64_t liec_group_norm_workspace(int32_t N, int64_t B, int64_t S, int64_t C, int64_t G) {
     if (!valid_norm(N, B, S, C, G)) return -1;
     if (B == 0 || S == 0) return 0;
-    const GnShape s = shape_of(N, B, S, C, G);
-    return gn_partials(s) * (int64_t)sizeof(float) + s.images * G * (int64_t)sizeof(float2);
+    return gn_run_bytes(C) + gn_chunk_scratch(N, B, S, C, G);
 }
 
 liec_status liec_group_norm(const liec_images* x, const liec_param* weight, const liec_param* bias, const liec_images* y, float* mean, float* rstd,
@@ -405,8 +487,8 @@ liec_status liec_group_norm(const liec_images* x, const liec_param* weight, cons
         for (const Span& v : written)
             if (&v < &w && spans_meet(v, w)) return LIEC_EINVAL;
     }
-    const GnForward a{shape_of(N, B, S, C, G), shape_of(N, B, S, C, G, kGnBlocks), images_of(x), images_of(y), param_of(weight, param_dtype), param_of(bias, param_dtype), mean, rstd,
-                      static_cast<float*>(workspace), eps, saved_of(saved), keeps((int64_t)N * B * S * C * size), activation, (hipStream_t)hip_stream};
+    const GnForward a{N, shape_of(N, B, S, C, G), shape_of(N, B, S, C, G, kGnBlocks), images_of(x), images_of(y), param_of(weight, param_dtype), param_of(bias, param_dtype), mean, rstd,
+                      reinterpret_cast<float*>(static_cast<char*>(workspace) + gn_run_bytes(C)), eps, saved_of(saved), keeps((int64_t)N * B * S * C * size), activation, (hipStream_t)hip_stream};
     if (dtype == LIEC_F32) gn_forward_of<float>(a);
     else if (dtype == LIEC_BF16) gn_forward_of<bf16>(a);
     else gn_forward_of<f16>(a);
@@ -461,17 +543,13 @@ liec_status liec_group_norm_backward(const liec_images* dy, const liec_images* x
         }
     }
     const hipStream_t st = (hipStream_t)hip_stream;
-    GnBackward a{shape_of(N, B, S, C, G), shape_of(N, B, S, C, G, kGnBlocks), images_of(dy), images_of(x), images_of(dx), saved_of(saved), param_of(weight, param_dtype), param_of(bias, param_dtype),
-                 param_of(dweight, param_dtype), param_of(dbias, param_dtype), mean, rstd, static_cast<float*>(workspace),
-                 keeps((int64_t)N * B * S * C * size), st};
-    int64_t parts = 0;
-    if (!empty && (dx || dweight || dbias))
-        parts = dtype == LIEC_F32 ? gn_backward_of<float>(a, activation) : dtype == LIEC_BF16 ? gn_backward_of<bf16>(a, activation) : gn_backward_of<f16>(a, activation);
-    if (dweight || dbias) {
-        const bool shared = N == 1 || (dweight ? dweight : dbias)->stride == 0;
-        if (!shared) parts /= N;
-        k_gn_param_grads<0><<<dim3((uint32_t)ceil_div(C, 32), shared ? 1u : (uint32_t)N, 2), kBlock, 0, st>>>(a.partial, parts, (uint32_t)C, a.dw, a.db);
-    }
+    const GnBackward a{N, shape_of(N, B, S, C, G), shape_of(N, B, S, C, G, kGnBlocks), images_of(dy), images_of(x), images_of(dx), saved_of(saved),
+                       param_of(weight, param_dtype), param_of(bias, param_dtype), param_of(dweight, param_dtype), param_of(dbias, param_dtype), mean, rstd,
+                       static_cast<double*>(workspace), reinterpret_cast<float*>(static_cast<char*>(workspace) + (empty ? 0 : gn_run_bytes(C))),
+                       empty ? 0 : need - gn_run_bytes(C), keeps((int64_t)N * B * S * C * size), st};
+    if (empty) gn_after_sums(a, 0, nullptr, true, true);
+    else if (dx || dweight || dbias)
+        dtype == LIEC_F32 ? gn_backward_of<float>(a, activation) : dtype == LIEC_BF16 ? gn_backward_of<bf16>(a, activation) : gn_backward_of<f16>(a, activation);
     return launched();
 }
 

@@ -14,7 +14,7 @@
 //
 // These are the kernels for images that no block holds: two passes over them, bound by memory and, with an activation, by arithmetic
 // beside it.  16 x 8 images of 56 x 56 x 256 bf16, ReLU: forward 36 us for the sums (5.7 TB/s), 5 for the groups, 78 for y
-// (5.2 TB/s of x and y); backward from a checkpoint 63 for the sums (4.9 TB/s), 5 + 5 for what comes of them, 96 for dx (5.4
+// (5.2 TB/s of x and y); backward from a checkpoint 63 for the sums (4.9 TB/s), 5 for what comes of them, 96 for dx (5.4
 // TB/s). 
 #pragma once
 #include <type_traits>
@@ -579,11 +579,11 @@ __global__ __launch_bounds__(kBlock) void k_gn_sums(GnShape s, const float* __re
     }
 }
 
-// Means of a and of a h over a group: pairs [images, G].
-template <int>
-__global__ __launch_bounds__(kBlock) void k_gn_means(GnShape s, const float* __restrict__ partial, LnParam weight, float2* __restrict__ means) {
-    for (int64_t g = gn_wave(); g < s.images * s.G; g += (int64_t)gridDim.x * (kBlock / 64)) {
-        const int64_t worker = g / s.G / s.B;
+// Means of a and of a h over a group: pairs [images, G].  Block `block` of `blocks`.
+__device__ __forceinline__ void gn_means(const GnShape& s, uint32_t block, uint32_t blocks, const float* __restrict__ partial, const LnParam& weight,
+                                         float2* __restrict__ means) {
+    for (int64_t g = (int64_t)block * (kBlock / 64) + (threadIdx.x >> 6); g < s.images * s.G; g += (int64_t)blocks * (kBlock / 64)) {
+        const int64_t worker = gn_worker(s, g / s.G);
         double sum_h = 0.0, sum_1 = 0.0;
         gn_each_part(s, g, [&](size_t at, uint32_t c, uint32_t) {
             const double w = weight.data ? (double)load_any(weight.data, worker * weight.stride + c, weight.type) : 1.0;
@@ -595,6 +595,49 @@ __global__ __launch_bounds__(kBlock) void k_gn_means(GnShape s, const float* __r
         const double n = (double)s.S * (double)s.per_group;
         if ((threadIdx.x & 63) == 0) means[g] = make_float2((float)(sum_1 / n), (float)(sum_h / n));
     }
+}
+
+// dw and db, the sums in fp64 of partial sums: `parts` of each of `workers` (one: all of them).  Sums that take several launches go through
+// `run`.
+struct GnParamGrads {
+    int64_t parts;
+    uint32_t workers, columns;         // columns: blocks of 32 channels
+    double* run;
+    bool first, last;
+    LnParam dw, db;
+};
+// 32 channels of one of the two gradients at a time per block, 8 threads to a channel.
+__device__ __forceinline__ void gn_param_grads(uint32_t C, uint32_t block, uint32_t blocks, const float* __restrict__ partial, const GnParamGrads& a) {
+    __shared__ double lds[8][32];
+    const uint32_t col = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    for (int64_t i = block; i < (int64_t)a.workers * a.columns * 2; i += blocks) {
+        const uint32_t which = (uint32_t)i & 1, half = (uint32_t)(i >> 1), worker = half / a.columns, c = (half - worker * a.columns) * 32 + col;
+        const LnParam& out = which ? a.db : a.dw;
+        if (!out.data) continue;
+        const float* const p = partial + (size_t)worker * a.parts * 2 * C + (which ? C : 0);
+        double sum = 0.0;
+        if (c < C) {
+#pragma unroll 4
+            for (int64_t q = slice; q < a.parts; q += 8) sum += (double)p[(size_t)q * 2 * C + c];
+        }
+        lds[slice][col] = sum;
+        __syncthreads();
+        if (slice == 0 && c < C) {
+            for (int q = 1; q < 8; ++q) sum += lds[q][col];
+            double* const so_far = a.run + (which ? C : 0u) + c;
+            if (!a.first) sum += *so_far;
+            if (a.last) store_any(out.data, (int64_t)worker * out.stride + c, out.type, (float)sum);
+            else *so_far = sum;
+        }
+        __syncthreads();
+    }
+}
+// Both in one launch: the first `blocks` blocks make the means.  Either may be left out (blocks = 0; no gradients asked for).
+template <int>
+__global__ __launch_bounds__(kBlock) void k_gn_after_sums(GnShape s, uint32_t blocks, const float* __restrict__ partial, LnParam weight, float2* __restrict__ means,
+                                                          GnParamGrads params) {
+    if (blockIdx.x < blocks) gn_means(s, blockIdx.x, blocks, partial, weight, means);
+    else gn_param_grads(s.C, blockIdx.x - blocks, gridDim.x - blocks, partial, params);
 }
 
 template <typename T, int V, int ACT, bool SAVED>
@@ -636,27 +679,6 @@ __global__ __launch_bounds__(kBlock) void k_gn_dx(GnShape s, bool keep, const fl
                 gn_store<T, V>(keep, first + u * step, k, d);
             }
         });
-    }
-}
-
-// dw and db of group blockIdx.y: the sum in fp64 of its `parts` partial sums, 32 channels per block, 8 threads to a channel.
-template <int>
-__global__ __launch_bounds__(kBlock) void k_gn_param_grads(const float* __restrict__ partial, int64_t parts, uint32_t C, LnParam dw, LnParam db) {
-    __shared__ double lds[8][32];
-    const LnParam& out = blockIdx.z ? db : dw;
-    if (!out.data) return;
-    const uint32_t col = threadIdx.x & 31, slice = threadIdx.x >> 5, c = blockIdx.x * 32 + col;
-    const float* const p = partial + (size_t)blockIdx.y * parts * 2 * C + (blockIdx.z ? C : 0);
-    double sum = 0.0;
-    if (c < C) {
-#pragma unroll 4
-        for (int64_t q = slice; q < parts; q += 8) sum += (double)p[(size_t)q * 2 * C + c];
-    }
-    lds[slice][col] = sum;
-    __syncthreads();
-    if (slice == 0 && c < C) {
-        for (int q = 1; q < 8; ++q) sum += lds[q][col];
-        store_any(out.data, (int64_t)blockIdx.y * out.stride + c, out.type, (float)sum);
     }
 }
 

@@ -424,6 +424,25 @@ def test_large_offsets():
         assert float((y[1, 0, -1, g * 4096:(g + 1) * 4096].double() - want).abs().max()) < 2 ** -8 * 6
 
 
+@pytest.mark.parametrize("N,B", [(3, 3001), (1, 9001), (2, 8500)])
+def test_many_images_in_parts(N, B):
+    """More partial sums than the scratch holds at a time: whole workers, or some of one worker's images; images that blocks hold,
+    and others."""
+    import paper_2402_11857_amd as pkg
+
+    say(f"case group norm of {N} x {B} images")
+    for S, C, G in ((2, 4096, 32), (2, 4100, 1)):            # 4100 channels in one group: no block holds it
+        x, dy, w, b = _inputs((N, B, S, C), "bf16", seed=21)
+        y, mean, rstd, saved = pkg.liec_group_norm(x, G, w, b, activation="silu", save=True)
+        check_forward(x, G, w, b, "silu", y, mean, rstd)
+        for shape, at in (((N, C), x), ((C,), saved)):
+            dw, db = torch.full(shape, 9.0, device=DEV), torch.full(shape, 9.0, device=DEV)
+            dx = pkg.liec_group_norm_backward(dy, at, mean, rstd, w, b, activation="silu", dweight=dw, dbias=db)
+            check_backward(dy, at if at is x else value(saved), mean, rstd, G, w, b, "silu", dx, dw, db)
+            assert torch.equal(dx[0, -1], pkg.liec_group_norm_backward(dy[:1, -1:], at[:1, -1:] if at is x else pkg.Checkpoint(*(t[:1, -1:].contiguous() for t in at)),
+                                                                       mean[:1, -1:].contiguous(), rstd[:1, -1:].contiguous(), w[:1], b[:1], activation="silu")[0, 0])
+
+
 def test_refusals():
     import paper_2402_11857_amd as pkg
 
