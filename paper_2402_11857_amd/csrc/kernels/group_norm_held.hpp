@@ -69,17 +69,24 @@ __device__ __forceinline__ T* gn_near(T* base, uint32_t bytes) {
     return reinterpret_cast<T*>(reinterpret_cast<byte*>(base) + bytes);
 }
 
-// Sum over the lanes of a wave that hold the same channels of the same image: those that differ in bits from..to of their number.
+// v of this lane plus v of another.
+template <int CTRL>
+__device__ __forceinline__ float gn_add_dpp(float v) {
+    return v + __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+}
+// Sum over the lanes of a wave that hold the same channels of the same image: those that differ in bits from..to of their number, the
+// same two for the whole launch.
 __device__ __forceinline__ float gn_rows_sum(float v, uint32_t from, uint32_t to) {
-    if (from <= 0 && to > 0) v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0xb1, 0xf, 0xf, true));    // quad_perm 1 0 3 2
-    if (from <= 1 && to > 1) v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x4e, 0xf, 0xf, true));    // quad_perm 2 3 0 1
-    if (from <= 2 && to > 2) v += __uint_as_float((uint32_t)__builtin_amdgcn_ds_swizzle((int)__float_as_uint(v), 4 << 10 | 0x1f));              // lane ^ 4
-    if (from <= 3 && to > 3) v += __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), 0x128, 0xf, 0xf, true));   // row_ror:8
-    if (from <= 4 && to > 4) {
+    const auto takes = [&](uint32_t bit) { return from <= bit && bit < to; };
+    if (takes(0)) v = gn_add_dpp<0xb1>(v);       // quad_perm 1 0 3 2
+    if (takes(1)) v = gn_add_dpp<0x4e>(v);       // quad_perm 2 3 0 1
+    if (takes(2)) v += __uint_as_float((uint32_t)__builtin_amdgcn_ds_swizzle((int)__float_as_uint(v), 4 << 10 | 0x1f));      // lane ^ 4
+    if (takes(3)) v = gn_add_dpp<0x128>(v);      // row_ror:8
+    if (takes(4)) {
         const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
-    if (from <= 5 && to > 5) {
+    if (takes(5)) {
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
     }
