@@ -147,7 +147,7 @@ GnShape shape_of(int64_t N, int64_t B, int64_t S, int64_t C, int64_t G, int64_t 
     return s;
 }
 int64_t gn_works_of(const GnShape& s) { return s.images * s.splits * s.tiles; }
-uint32_t gn_group_blocks(const GnShape& s) { return grid_of(ceil_div(s.images * s.G, kBlock / 64)); }
+uint32_t gn_group_blocks(const GnShape& s) { return grid_of(s.images * s.G <= kGnFewGroups ? s.images * s.G : ceil_div(s.images * s.G, kBlock / 64)); }
 int64_t gn_partials(const GnShape& s) { return s.images * s.splits * 2 * (int64_t)s.C; }
 GnImages images_of(const liec_images* x) { return x && x->data ? GnImages{x->data, x->worker_stride, x->image_stride, x->row_stride} : GnImages{nullptr, 0, 0, 0}; }
 

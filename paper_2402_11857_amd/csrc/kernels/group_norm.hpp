@@ -293,38 +293,65 @@ __global__ __launch_bounds__(kBlock) void k_gn_stats(GnShape s, GnImages x, floa
     }
 }
 
-// A wave goes over what an image's strips left of a group's channels: neighbouring lanes on neighbouring channels.
+// What an image's strips left of a group's channels, neighbouring lanes on neighbouring channels: of every `parts`-th set of strips.
 template <typename F>
-__device__ __forceinline__ void gn_each_part(const GnShape& s, int64_t group, F f) {
+__device__ __forceinline__ void gn_each_part(const GnShape& s, int64_t group, uint32_t part, uint32_t parts, F f) {
     const int64_t image = group / s.G;
     const uint32_t first = (uint32_t)(group - image * s.G) * s.per_group, lane = threadIdx.x & 63;
-    const uint32_t wide_log = s.per_group >= 64 ? 6 : 32 - __clz((int)s.per_group), wide = 1u << wide_log;
+    const uint32_t wide_log = s.per_group >= 64 ? 6 : 32 - __clz((int)s.per_group), wide = 1u << wide_log, step = 64u >> wide_log;
 #pragma unroll 4
-    for (uint32_t split = lane >> wide_log; split < s.splits; split += 64 >> wide_log)
+    for (uint32_t split = part * step + (lane >> wide_log); split < s.splits; split += parts * step)
         for (uint32_t c = lane & (wide - 1); c < s.per_group; c += wide) f((size_t)(image * s.splits + split) * 2 * s.C + first + c, first + c, split);
 }
-
-__device__ __forceinline__ int64_t gn_wave() { return (int64_t)blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6); }
+// Two sums over each group in fp64, added up by a wave, or, of few groups, by a block: add(group, part, parts, two sums) for a lane's share,
+// done(group, both) on one lane.  Block `block` of `blocks`.  A few groups are many strips each, one load after the other.  Whole calls in us,
+// a wave per group and a block: 10 groups (5 images of 2466 x 66) 27 and 17; 640 (784 x 250) 25.1 and 24.5, backward 32.8 and 31.7; 1024
+// (3136 x 66) 160 and 160; 2048 (196 x 500) 55.7 and 56.4; 20 480 107 and 120.
+constexpr int64_t kGnFewGroups = 1024;
+template <typename A, typename D>
+__device__ __forceinline__ void gn_each_group_sums(const GnShape& s, uint32_t block, uint32_t blocks, A add, D done) {
+    __shared__ double lds[kBlock / 64][2];
+    constexpr uint32_t waves = kBlock / 64;
+    const uint32_t wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const bool few = s.images * s.G <= kGnFewGroups;
+    for (int64_t g = few ? block : (int64_t)block * waves + wave; g < s.images * s.G; g += few ? blocks : (int64_t)blocks * waves) {
+        double a = 0.0, b = 0.0;
+        add(g, few ? wave : 0u, few ? waves : 1u, a, b);
+        a = wave_sum(a);
+        b = wave_sum(b);
+        if (few) {
+            if (lane == 0) lds[wave][0] = a, lds[wave][1] = b;
+            __syncthreads();
+            a = lds[0][0], b = lds[0][1];
+            for (uint32_t w = 1; w < waves; ++w) a += lds[w][0], b += lds[w][1];
+            __syncthreads();
+        }
+        if (lane == 0 && (!few || wave == 0)) done(g, a, b);
+    }
+}
 
 template <int>
 __global__ __launch_bounds__(kBlock) void k_gn_groups(GnShape s, const float* __restrict__ partial, float eps, float* __restrict__ mean, float* __restrict__ rstd) {
-    for (int64_t g = gn_wave(); g < s.images * s.G; g += (int64_t)gridDim.x * (kBlock / 64)) {
+    // values around one of the group's means
+    const auto around = [&](int64_t g) {
         const int64_t image = g / s.G;
-        const double p = (double)partial[(size_t)image * s.splits * 2 * s.C + (uint32_t)(g - image * s.G) * s.per_group];
-        double sum = 0.0, squares = 0.0;
-        gn_each_part(s, g, [&](size_t at, uint32_t, uint32_t split) {
-            const double n = (double)min(s.per, s.S - split * s.per), d = (double)partial[at] - p;
-            sum += n * d;
-            squares += (double)partial[at + s.C] + n * d * d;
-        });
-        sum = wave_sum(sum);
-        squares = wave_sum(squares);
-        const double n = (double)s.S * (double)s.per_group, d = sum / n, var = (squares - d * sum) / n;
-        if ((threadIdx.x & 63) == 0) {
-            mean[g] = (float)(p + d);
+        return (double)partial[(size_t)image * s.splits * 2 * s.C + (uint32_t)(g - image * s.G) * s.per_group];
+    };
+    gn_each_group_sums(
+        s, blockIdx.x, gridDim.x,
+        [&](int64_t g, uint32_t part, uint32_t parts, double& sum, double& squares) {
+            const double p = around(g);
+            gn_each_part(s, g, part, parts, [&](size_t at, uint32_t, uint32_t split) {
+                const double n = (double)min(s.per, s.S - split * s.per), d = (double)partial[at] - p;
+                sum += n * d;
+                squares += (double)partial[at + s.C] + n * d * d;
+            });
+        },
+        [&](int64_t g, double sum, double squares) {
+            const double n = (double)s.S * (double)s.per_group, d = sum / n, var = (squares - d * sum) / n;
+            mean[g] = (float)(around(g) + d);
             rstd[g] = (float)(1.0 / sqrt((var > 0.0 ? var : var - var) + (double)eps));
-        }
-    }
+        });
 }
 
 // Bits of the largest magnitude of a checkpoint's group of columns: the lanes that share it.
@@ -582,19 +609,20 @@ __global__ __launch_bounds__(kBlock) void k_gn_sums(GnShape s, const float* __re
 // Means of a and of a h over a group: pairs [images, G].  Block `block` of `blocks`.
 __device__ __forceinline__ void gn_means(const GnShape& s, uint32_t block, uint32_t blocks, const float* __restrict__ partial, const LnParam& weight,
                                          float2* __restrict__ means) {
-    for (int64_t g = (int64_t)block * (kBlock / 64) + (threadIdx.x >> 6); g < s.images * s.G; g += (int64_t)blocks * (kBlock / 64)) {
-        const int64_t worker = gn_worker(s, g / s.G);
-        double sum_h = 0.0, sum_1 = 0.0;
-        gn_each_part(s, g, [&](size_t at, uint32_t c, uint32_t) {
-            const double w = weight.data ? (double)load_any(weight.data, worker * weight.stride + c, weight.type) : 1.0;
-            sum_h += w * (double)partial[at];
-            sum_1 += w * (double)partial[at + s.C];
+    gn_each_group_sums(
+        s, block, blocks,
+        [&](int64_t g, uint32_t part, uint32_t parts, double& sum_h, double& sum_1) {
+            const int64_t worker = gn_worker(s, g / s.G);
+            gn_each_part(s, g, part, parts, [&](size_t at, uint32_t c, uint32_t) {
+                const double w = weight.data ? (double)load_any(weight.data, worker * weight.stride + c, weight.type) : 1.0;
+                sum_h += w * (double)partial[at];
+                sum_1 += w * (double)partial[at + s.C];
+            });
+        },
+        [&](int64_t g, double sum_h, double sum_1) {
+            const double n = (double)s.S * (double)s.per_group;
+            means[g] = make_float2((float)(sum_1 / n), (float)(sum_h / n));
         });
-        sum_h = wave_sum(sum_h);
-        sum_1 = wave_sum(sum_1);
-        const double n = (double)s.S * (double)s.per_group;
-        if ((threadIdx.x & 63) == 0) means[g] = make_float2((float)(sum_1 / n), (float)(sum_h / n));
-    }
 }
 
 // dw and db, the sums in fp64 of partial sums: `parts` of each of `workers` (one: all of them).  Sums that take several launches go through
