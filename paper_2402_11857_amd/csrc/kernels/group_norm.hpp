@@ -40,15 +40,15 @@ struct GnShape {
 };
 
 // ---- activation ------------------------------------------------------------------------------------------------------
-// exp(-z), at most 2^126.  For results of 16 bits the product's rounding error stays, |z| u of the exponential; for fp32 it is put
-// right, to about 2 u.
+// exp(-z), an infinity from 2^128 on, whose reciprocal is the limit, 0 (a reciprocal under 2^-126 may come as 0 too).  For results of 16
+// bits the product's rounding error stays, |z| u of the exponential; for fp32 it is put right, to about 2 u.
 template <typename T>
 __device__ __forceinline__ float exp_minus(float z) {
     const float log2e = 1.44269502f, rest = 1.92596299e-8f;              // their sum is log2(e)
-    const float t = -z * log2e, e = __builtin_amdgcn_exp2f(fminf(t, 126.f));
+    const float t = -z * log2e, e = __builtin_amdgcn_exp2f(t);
     if (sizeof(T) == 2) return e;
     const float off = __fmaf_rn(-z, rest, __fmaf_rn(-z, log2e, -t));
-    return fabsf(t) < 126.f ? __fmaf_rn(e, off * 0.693147181f, e) : e;
+    return fabsf(t) < 128.f ? __fmaf_rn(e, off * 0.693147181f, e) : e;
 }
 
 template <typename T, int ACT>
