@@ -76,7 +76,8 @@ int64_t liec_group_norm_workspace(int32_t N, int64_t B, int64_t S, int64_t C, in
  *   1 <= N <= 65535, 0 <= B < 2^31, 0 <= S < 2^31 (nothing in an image: nothing to do), 1 <= C <= 2^20, G a divisor of C, at most
  *   2^40 values, eps >= 0 and finite; no value lies further than 2^40 values from the first
  * y may be x itself (same pointer and strides); otherwise they share no memory, and neither do y's rows with one another, or with
- * weight or bias.  A group that holds an infinity or a NaN gets NaN.
+ * weight or bias.  A group that holds an infinity or a NaN gets NaN, and so may one whose values add up beyond the largest fp32 number;
+ * where only the squares of their distances from the mean do (distances of 1e19, say), rstd is 0 and y = act(bias).
  */
 liec_status liec_group_norm(const liec_images *x, const liec_param *weight, const liec_param *bias, const liec_images *y, float *mean, float *rstd,
                             const liec_checkpoint *saved, int32_t N, int64_t B, int64_t S, int64_t C, int64_t G, float eps,

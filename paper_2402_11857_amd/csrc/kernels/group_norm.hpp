@@ -207,11 +207,12 @@ __device__ __forceinline__ void gn_store_channels(const GnShape& s, const GnWork
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------------------
-// Mean and squares around it of n and n2 values, put together.
+// Mean and squares around it of n and n2 values, put together.  Where one of the two has no values the square of their means' distance does not
+// count, and may be beyond fp32.
 __device__ __forceinline__ void gn_join(float n, float& mean, float& squares, float n2, float mean2, float squares2) {
-    const float all = n + n2, share = all > 0.f ? n2 / all : 0.f, d = mean2 - mean;
+    const float all = n + n2, share = all > 0.f ? n2 / all : 0.f, d = mean2 - mean, weight = n * share;
     mean = __fmaf_rn(d, share, mean);
-    squares += __fmaf_rn(d * d, n * share, squares2);
+    squares += weight > 0.f ? __fmaf_rn(d * d, weight, squares2) : squares2;
 }
 
 // Mean and squares around it of each channel over a strip of an image's positions.  A thread takes its values around the mean p of its
