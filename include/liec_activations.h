@@ -71,7 +71,7 @@ int64_t liec_group_norm_workspace(int32_t N, int64_t B, int64_t S, int64_t C, in
  * liec_group_norm: the C channels of an image fall into G groups of C / G neighbours; for every image and group, over its S positions
  * and its channels, mu = mean(x), rstd = 1 / sqrt(mean((x - mu)^2) + eps), and y = act((x - mu) * rstd * weight + bias).
  *   weight, bias [N, C] as in liec_layer_norm (stride 0: one vector for all workers; none: 1 and 0)
- *   mean, rstd   DEVICE fp32 [N, B, G] contiguous, for the backward pass; memory of their own
+ *   mean, rstd   DEVICE fp32 [N, B, G] contiguous, for the backward pass; memory of their own; left as they are where S = 0
  *   saved        NULL, or a checkpoint of x as rows [N, B * S, C], written in the same pass; memory of its own
  *   1 <= N <= 65535, 0 <= B < 2^31, 0 <= S < 2^31 (nothing in an image: nothing to do), 1 <= C <= 2^20, G a divisor of C, at most
  *   2^40 values, eps >= 0 and finite; no value lies further than 2^40 values from the first

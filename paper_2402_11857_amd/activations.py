@@ -60,8 +60,9 @@ def liec_group_norm(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor]
                     activation: str = "none", out: Optional[torch.Tensor] = None, save: bool = False) -> Tuple:
     """Group normalisation of images [N, B, ..., C], channels last, over an image's positions and the C / groups neighbouring
     channels of a group, scaled by weight, shifted by bias and passed through an activation function ("none", "relu", "silu"):
-    (y, mean, rstd), the latter two float32 [N, B, groups].  weight and bias: [C], or [N, C] for the N workers (columns of a
-    models tensor, say).  `out` may be x.  With save=True a checkpoint of x, written in the same pass, comes as the fourth."""
+    (y, mean, rstd), the latter two float32 [N, B, groups] (NaN for images without positions).  weight and bias: [C], or [N, C] for
+    the N workers (columns of a models tensor, say).  `out` may be x.  With save=True a checkpoint of x, written in the same
+    pass, comes as the fourth."""
     r = native().group_norm(x, groups, weight, bias, eps, _activation(activation), out, bool(save))
     first = out if out is not None else r[0]
     return (first, r[1], r[2], Checkpoint(r[3], r[4])) if save else (first, r[1], r[2])

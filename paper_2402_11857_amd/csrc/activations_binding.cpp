@@ -1,6 +1,8 @@
 // Python side of include/liec_activations.h: argument checks, outputs, scratch and the call, in one step per operator.
 #include <torch/csrc/Dtype.h>
 
+#include <limits>
+
 #include "binding_common.hpp"
 #include "liec_activations.h"
 
@@ -149,6 +151,8 @@ PyObject* group_norm(PyObject* const* a) {           // x, groups, weight, bias,
     const int64_t bytes = p_group_norm_workspace(s.N, s.B, s.S, s.C, s.G);
     const at::Tensor ws = scratch(bytes, x, "images"), y = out ? *out : new_tensor(x.sizes(), x.scalar_type(), x);
     const at::Tensor mean = new_tensor({s.N, s.B, s.G}, at::kFloat, x), rstd = new_tensor({s.N, s.B, s.G}, at::kFloat, x);
+    if (!s.S)                          // means of nothing: the library leaves them alone
+        for (const at::Tensor* t : {&mean, &rstd}) t->fill_(std::numeric_limits<float>::quiet_NaN());
     const bool save = a[7] == Py_True;
     const Checkpoint saved = save ? new_checkpoint(x) : Checkpoint{};
     const liec_checkpoint raw = save ? saved.raw() : liec_checkpoint{nullptr, nullptr};
