@@ -67,29 +67,61 @@ void run_load(const Saved& from, LnRows y, int64_t N, int64_t R, int64_t C, hipS
 }
 
 // ---- group normalisation ---------------------------------------------------------------------------------------------
-// Images as an operand: the runs of each worker's images, or of all of them where workers follow one another.
+// Images as an operand: runs of channels at up to three distances, in the order of these.  What follows one another is one, two
+// distances are a span, and of three the largest is between groups of runs (or, where that would be very many groups, that of the
+// fewest).
 struct ImageSpans {
-    int64_t first, wide, many;         // bytes between groups of runs
+    int64_t first, wide, many;         // bytes between groups, 0 for a single one
     int64_t len, s, n, t, m;           // a group: m times at distances t, n runs of len at distances s
     Span at(int64_t i) const { return span_of((const void*)(first + i * wide), len, s, n, t, m); }
 };
+constexpr int64_t kImageGroups = (int64_t)1 << 16;
 ImageSpans image_spans(const liec_images* x, int64_t N, int64_t B, int64_t S, int64_t C, int64_t size) {
-    const int64_t w = x->worker_stride * size, b = x->image_stride * size, r = x->row_stride * size, at = (int64_t)(uintptr_t)x->data;
-    if (N == 1 || w == B * b) return {at, 0, 1, C * size, r, S, b, N * B};
-    if (B == 1 || b == S * r) return {at, 0, 1, C * size, r, B * S, w, N};
-    return {at, w, N, C * size, r, S, b, B};
+    struct {
+        int64_t stride, n;
+    } d[3] = {{x->row_stride * size, S}, {x->image_stride * size, B}, {x->worker_stride * size, N}};
+    ImageSpans r{(int64_t)(uintptr_t)x->data, 0, 1, C * size, 0, 1, 0, 1};
+    int dims = 0;
+    for (const auto& e : d) {
+        if (e.n == 1 || e.stride == 0) continue;
+        if (e.stride < 0) r.first += (e.n - 1) * e.stride;
+        d[dims++] = {llabs(e.stride), e.n};
+    }
+    std::sort(d, d + dims, [](const auto& a, const auto& b) { return a.stride < b.stride; });
+    for (int i = 1; i < dims;) {
+        if (d[i].stride != d[i - 1].n * d[i - 1].stride) {
+            ++i;
+            continue;
+        }
+        d[i - 1].n *= d[i].n;
+        for (int k = i + 1; k < dims; ++k) d[k - 1] = d[k];
+        --dims;
+    }
+    if (dims == 3) {
+        if (d[2].n > kImageGroups) std::swap(d[2], *std::min_element(d, d + 3, [](const auto& a, const auto& b) { return a.n < b.n; }));
+        r.wide = d[2].stride, r.many = d[2].n;
+    }
+    if (dims > 0) r.s = d[0].stride, r.n = d[0].n;
+    if (dims > 1) r.t = d[1].stride, r.m = d[1].n;
+    return r;
 }
-bool images_meet(const ImageSpans& a, const Span& p) {
-    int64_t steps = kSpanSteps;
-    for (int64_t i = 0; i < a.many; ++i)
+// Only groups that come near one another are looked at: a few for each where operands lie between one another.
+bool images_meet(const ImageSpans& a, const Span& p, int64_t& steps) {
+    const Span box = a.at(0);
+    if (box.len <= 0 || p.len <= 0) return false;
+    for (int64_t i = first_ending_after(p.lo - box.lo, box.hi - box.lo, a.wide); i < a.many && box.lo + i * a.wide < p.hi; ++i)
         if (--steps < 0 || spans_meet(a.at(i), p, steps)) return true;
     return false;
 }
+bool images_meet(const ImageSpans& a, const Span& p) {
+    int64_t steps = kSpanSteps;
+    return images_meet(a, p, steps);
+}
 bool images_meet(const ImageSpans& a, const ImageSpans& b) {
     int64_t steps = kSpanSteps;
-    for (int64_t i = 0; i < a.many; ++i)
-        for (int64_t j = 0; j < b.many; ++j)
-            if (--steps < 0 || spans_meet(a.at(i), b.at(j), steps)) return true;
+    const ImageSpans &few = a.many <= b.many ? a : b, &other = a.many <= b.many ? b : a;
+    for (int64_t i = 0; i < few.many; ++i)
+        if (--steps < 0 || images_meet(other, few.at(i), steps)) return true;
     return false;
 }
 // Rows that are written must not share memory: each distance spans what the narrower ones cover.
