@@ -413,7 +413,6 @@ void gn_backward_of(const GnBackward& a, int act) {
 bool valid_act(int a) { return a == LIEC_ACT_NONE || a == LIEC_ACT_RELU || a == LIEC_ACT_SILU; }
 
 // ---- weight gradients ------------------------------------------------------------------------------------------------
-constexpr int64_t kWgChain = 8192;     // rows that are added up in fp32
 constexpr int64_t kWgStep = 64;        // rows that a split is a multiple of
 constexpr int64_t kWgBlocks = 512;     // that a launch should have at least, where there are rows for them
 
@@ -432,7 +431,7 @@ WgShape weight_shape(int64_t N, int64_t R, int64_t O, int64_t C) {
     s.tiles_o = (uint32_t)ceil_div(O, tile), s.tiles_c = (uint32_t)ceil_div(C, tile);
     const int64_t blocks = N * s.tiles_o * (int64_t)s.tiles_c;
     int64_t splits = std::max<int64_t>(1, std::min(kWgBlocks / blocks, R / (4 * kWgStep)));
-    splits = std::max(splits, ceil_div(R, kWgChain));
+    splits = std::max(splits, ceil_div(R, (int64_t)kWgChain));
     s.per = std::max(kWgStep, ceil_div(ceil_div(R, splits), kWgStep) * kWgStep);
     s.splits = (uint32_t)std::max<int64_t>(1, ceil_div(R, s.per));
     return s;

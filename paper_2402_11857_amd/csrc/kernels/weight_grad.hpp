@@ -101,6 +101,12 @@ struct WgTile {
     static_assert(BK % a_rows == 0 && (BK % b_rows == 0 || b_rows % BK == 0), "whole loads");
 };
 
+// The bias is added up in fp32 over at most so many rows of a thread (a step's, where rows are at distances of 16 bytes), and in fp64 beyond.
+// Chains over whole splits were off by up to 440 u of rows of one sign (2048 rows, each three bf16 numbers), those of 256 additions
+// are by less than 86.
+constexpr int kWgBiasChain = 256;
+constexpr int kWgChain = 8192;         // rows of a split, at most: products of them are added up in fp32
+
 struct WgWork {
     uint32_t tile_o, tile_c, split, worker;
 };
@@ -126,6 +132,8 @@ __global__ __launch_bounds__(WM* WN * 64) void k_weight_grad(WgShape s, LnRows d
     typedef WgTile<T, BM, BN, BK, WM, WN> W;
     constexpr int P = W::P;
     __shared__ __attribute__((aligned(16))) uint16_t lds[2][W::values];
+    constexpr bool once = W::a_rows * kWgBiasChain >= kWgChain;          // a thread's rows of a split are one chain
+    __shared__ double totals[once ? 1 : W::threads / 64][BM];            // of a wave's rows
     const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const uint32_t wave_m = wave / WN * (BM / WM), wave_n = wave % WN * (BN / WN);
     const uint32_t a_col = tid % W::a_lanes * 8, a_row = tid / W::a_lanes, b_col = tid % W::b_lanes * 16, b_row = tid / W::b_lanes;
@@ -229,6 +237,18 @@ __global__ __launch_bounds__(WM* WN * 64) void k_weight_grad(WgShape s, LnRows d
             }
         };
 
+        bool some = false;             // totals there
+        auto add_up = [&] {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float v = sums[j];
+#pragma unroll
+                for (int off = W::a_lanes; off < 64; off <<= 1) v += __shfl_xor(v, off);
+                if (lane < (uint32_t)W::a_lanes) totals[wave][a_col + j] = some ? totals[wave][a_col + j] + (double)v : (double)v;
+                sums[j] = 0.f;
+            }
+            some = true;
+        };
         v16f acc[W::TM][W::TN];
 #pragma unroll
         for (int m = 0; m < W::TM; ++m)
@@ -241,8 +261,15 @@ __global__ __launch_bounds__(WM* WN * 64) void k_weight_grad(WgShape s, LnRows d
         const uint32_t k_at = lane >> 5 << 3 | (lane >> 2 & 3), col_at = (lane & 16) | (lane & 3) << 2;
         fetch(r0);
         int buffer = 0;
+        [[maybe_unused]] int left = kWgBiasChain / W::a_loads;
         for (int64_t r = r0; r < r1; r += BK) {
             stage(lds[buffer]);
+            if constexpr (!once) {
+                if (bias && --left == 0) {
+                    add_up();
+                    left = kWgBiasChain / W::a_loads;
+                }
+            }
             __syncthreads();
             if (r + BK < r1) fetch(r + BK);
             const uint16_t* const at = lds[buffer];
@@ -295,10 +322,13 @@ __global__ __launch_bounds__(WM* WN * 64) void k_weight_grad(WgShape s, LnRows d
             __syncthreads();
             for (uint32_t t = tid; t < (uint32_t)BM; t += W::threads) {
                 if (o0 + t >= s.O) continue;
-                float v = 0.f;
+                std::conditional_t<once, float, double> v = 0;
                 for (int i = 0; i < W::a_rows; ++i) v += rows[i * BM + t];
-                if (part) part[s.O * s.C + o0 + t] = v;
-                else store_any(db.data, (int64_t)worker * db.stride + o0 + t, db.type, v);
+                if constexpr (!once) {
+                    for (int i = 0; some && i < W::threads / 64; ++i) v += totals[i][t];
+                }
+                if (part) part[s.O * s.C + o0 + t] = (float)v;
+                else store_any(db.data, (int64_t)worker * db.stride + o0 + t, db.type, (float)v);
             }
             __syncthreads();
         }
@@ -468,6 +498,15 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_weight_grad_aligned(WgShape 
                 }
             }
         };
+        // every step, without a branch: one per 256 rows took 5 of 64 us more, where a quarter of the blocks add up the bias
+        double total[W::TM] = {};
+        auto add_up = [&] {
+#pragma unroll
+            for (int m = 0; m < W::TM; ++m) {
+                total[m] += (double)sums[m];
+                sums[m] = 0.f;
+            }
+        };
         // A step multiplies one buffer while the next is filled: dy's rows are on their way from its start (bf16) or, like x's, from
         // the end of the step before, and x is widened and stored beside the last products.
         auto steps_of = [&](auto with_bias) {
@@ -510,6 +549,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_weight_grad_aligned(WgShape 
                 }
                 if constexpr (P > 1) fetch_a(r + 2 * BK);
                 fetch_b(r + 2 * BK);
+                if (with_bias) add_up();
                 wg_wait<P == 1 ? 2 * W::b_loads : -1>();
                 buffer ^= 1;
             }
@@ -538,19 +578,16 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_weight_grad_aligned(WgShape 
         else if (dw.type == kF32) store([&](int64_t o, int64_t c, float v) { static_cast<float*>(dw.data)[out + o * dw.row + c] = v; });
         else store([&](int64_t o, int64_t c, float v) { store_any(dw.data, out + o * dw.row + c, dw.type, v); });
         if (bias) {
-            float* const rows = reinterpret_cast<float*>(lds[0]);        // [WN][BM]
+            double* const rows = reinterpret_cast<double*>(lds[0]);      // [2 WN][BM]
 #pragma unroll
-            for (int m = 0; m < W::TM; ++m) {
-                const float v = sums[m] + __shfl_xor(sums[m], 32);
-                if (lane < 32) rows[wave % WN * BM + wave_m + 32 * m + lane] = v;
-            }
+            for (int m = 0; m < W::TM; ++m) rows[(wave % WN * 2 + (lane >> 5)) * BM + wave_m + 32 * m + (lane & 31)] = total[m];
             __syncthreads();
             for (uint32_t t = tid; t < (uint32_t)BM; t += W::threads) {
                 if (o0 + t >= s.O) continue;
-                float v = 0.f;
-                for (int i = 0; i < WN; ++i) v += rows[i * BM + t];
-                if (part) part[s.O * s.C + o0 + t] = v;
-                else store_any(db.data, (int64_t)w.worker * db.stride + o0 + t, db.type, v);
+                double v = 0.0;
+                for (int i = 0; i < 2 * WN; ++i) v += rows[i * BM + t];
+                if (part) part[s.O * s.C + o0 + t] = (float)v;
+                else store_any(db.data, (int64_t)w.worker * db.stride + o0 + t, db.type, (float)v);
             }
         }
         __syncthreads();
