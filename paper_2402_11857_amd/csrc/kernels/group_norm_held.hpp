@@ -327,6 +327,21 @@ __global__ __launch_bounds__(kGnHeldMost) void k_gn_held_backward(GnShape s, GnH
                     grad[k].hide();
                 }
             if (__builtin_expect(near, 0)) {
+                // weights out of memory again, one row after the other: registers are full
+                near = false;
+                float w[8];
+                gn_param<8>(weight, gn_worker(s, p.image), p.k.c, 1.f, w);
+#pragma unroll
+                for (int k = 0; k < K; ++k)
+                    if (k < rows) {
+                        float d[8];
+                        raw[k].center(p.k, t.mu, d);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) near |= gn_undecided(__fmaf_rn(d[j], zw[j], t.b[j]), d[j], w[j], t.b[j]);
+                        raw[k].hide();
+                    }
+            }
+            if (__builtin_expect(near, 0)) {
                 // value by value, everything read again: registers are full, and these are a few in a million
 #pragma unroll 1
                 for (uint32_t i = 0; i < h.rows * 8; ++i) {

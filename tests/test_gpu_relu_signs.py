@@ -1,0 +1,118 @@
+"""Where a ReLU's gradient is decided in 64 bits: on every path and at every place of a vector, and only where something is to decide."""
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(__file__))
+from _activations import activations, value  # noqa: E402
+from _gpu import DEV, GPU_MARKS, say  # noqa: E402
+from _train import DTYPES, U32, generator  # noqa: E402
+from test_gpu_group_norm import check_backward  # noqa: E402
+
+pytestmark = GPU_MARKS
+# images that a block holds and images in two passes, each with channels that are a multiple of 8 and others, and fewer than 8
+PATHS = [((2, 3, 50, 64), 4), ((2, 3, 50, 90), 9), ((2, 1, 3000, 64), 4), ((1, 2, 3000, 90), 9), ((2, 2, 300, 6), 3), ((1, 1, 2500, 1031), 1)]
+
+
+@pytest.mark.parametrize("shape,G", PATHS)
+@pytest.mark.parametrize("kept", ["x", "checkpoint"])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_signs_next_to_zero(shape, G, kept, dtype):
+    import paper_2402_11857_amd as pkg
+
+    say(f"case ReLU next to zero {shape} {dtype} from {kept}")
+    N, B, S, C = shape
+    gen = generator(31)
+    x = activations(shape, dtype, 30)
+    dy = (0.1 * torch.randn(shape, generator=gen, device=DEV)).to(DTYPES[dtype])
+    w = 1 + 0.2 * torch.randn(N, C, generator=gen, device=DEV)
+    _, mean, rstd, saved = pkg.liec_group_norm(x, G, save=True)
+    at = value(saved) if kept == "checkpoint" else x.double()
+    wide = lambda t: t.double().repeat_interleave(C // G, -1)[:, :, None]                # noqa: E731
+    h = (at - wide(mean)) * wide(rstd)
+    # biases that put one position of every channel next to zero
+    b = -(h[:, B - 1, S // 3] * w.double()).float()
+    z = h * w.double()[:, None, None] + b.double()[:, None, None]
+    near = z.abs() < 4 * U32 * b.double().abs()[:, None, None]
+    assert near.sum() >= 0.9 * N * C
+    for odd in (0, 1):
+        assert (z[..., odd::2][near[..., odd::2]] > 0).any() and (z[..., odd::2][near[..., odd::2]] < 0).any()
+    dw, db = torch.empty_like(w), torch.empty_like(w)
+    dx = pkg.liec_group_norm_backward(dy, saved if kept == "checkpoint" else x, mean, rstd, w, b, activation="relu", dweight=dw, dbias=db)
+    check_backward(dy, at, mean, rstd, G, w, b, "relu", dx, dw, db)
+
+
+@pytest.mark.parametrize("shape,G", PATHS)
+@pytest.mark.parametrize("kept", ["x", "checkpoint"])
+def test_products_too_small_for_32_bits(shape, G, kept):
+    """Without biases z is 0 in fp32 where the product of deviation, rstd and weight is too small for it: its sign still counts.  Weights
+    of zero, and values that are the mean, have none."""
+    import paper_2402_11857_amd as pkg
+
+    say(f"case ReLU of products too small {shape} from {kept}")
+    N, C = shape[0], shape[-1]
+    gen = generator(33)
+    dy = torch.randn(shape, generator=gen, device=DEV)
+    w = torch.where(torch.rand(N, C, generator=gen, device=DEV) < 0.5, 2e-38, -2e-38)
+    w[:, ::3] = 0.0
+    zero = torch.zeros_like(w)
+    for size, eps in ((1e-12, 1.0), (1e12, 1e-5)):
+        x = size * torch.randn(shape, generator=gen, device=DEV)
+        _, mean, rstd, saved = pkg.liec_group_norm(x, G, eps=eps, save=True)
+        at = value(saved) if kept == "checkpoint" else x.double()
+        wide = lambda t: t.double().repeat_interleave(C // G, -1)[:, :, None]            # noqa: E731
+        h = (at - wide(mean)) * wide(rstd)
+        for b in (zero, None):
+            dw, db = torch.full_like(w, 9.0), torch.full_like(w, 9.0)
+            pkg.liec_group_norm_backward(dy, saved if kept == "checkpoint" else x, mean, rstd, w, zero, activation="relu", dweight=dw, dbias=db)
+            assert not db[:, ::3].any() and (h[:, :, :, 1] * w[:, None, None, 1].double() > 0).any()
+            check_backward(dy, at, mean, rstd, G, w, b, "relu", None, dw, db)
+    for b in (zero, None):
+        x = torch.full(shape, 2.0, device=DEV)
+        _, mean, rstd, saved = pkg.liec_group_norm(x, G, save=True)
+        db = torch.full_like(w, 9.0)
+        dx = pkg.liec_group_norm_backward(dy, saved if kept == "checkpoint" else x, mean, rstd, w, b, activation="relu", dbias=db)
+        assert not db.any() and not dx.any()
+
+
+def _time(run):
+    """Shortest of a few runs, in milliseconds."""
+    times = []
+    for _ in range(9):
+        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        begin.record()
+        for _ in range(5):
+            run()
+        end.record()
+        end.synchronize()
+        times.append(begin.elapsed_time(end))
+    return min(times)
+
+
+@pytest.mark.parametrize("shape,G", [((8, 8, 196, 512), 16), ((8, 8, 3136, 64), 8)])
+@pytest.mark.parametrize("kept", ["x", "checkpoint"])
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_nothing_to_decide_costs_little(shape, G, kept, dtype):
+    """Channels whose weight and bias are zero, and images whose values are all the mean, take little more time than others: deciding
+    each of them in 64 bits took 1.6 to 2.6 times as long, looking whether there is something to decide 1.1 to 1.35 times."""
+    import paper_2402_11857_amd as pkg
+
+    say(f"case ReLU with nothing to decide {shape} {dtype} from {kept}")
+    N, C = shape[0], shape[-1]
+    gen = generator(35)
+    dy = torch.randn(shape, generator=gen, device=DEV).to(DTYPES[dtype])
+    w, b = 1 + 0.2 * torch.randn(N, C, generator=gen, device=DEV), 0.2 * torch.randn(N, C, generator=gen, device=DEV)
+    dw, db, dx = torch.empty_like(w), torch.empty_like(w), torch.empty_like(dy)
+    x = activations(shape, dtype, 34)
+
+    def timed(x, w, b):
+        _, mean, rstd, saved = pkg.liec_group_norm(x, G, save=True)
+        at = saved if kept == "checkpoint" else x
+        return _time(lambda: pkg.liec_group_norm_backward(dy, at, mean, rstd, w, b, activation="relu", dx=dx, dweight=dw, dbias=db))
+
+    zero = torch.zeros_like(w)
+    usual, none, flat = timed(x, w, b), timed(x, zero, zero), timed(torch.full_like(x, 2.0), w, zero)
+    say(f"ms of 5 calls: {usual:.3f}, no weights {none:.3f}, flat images {flat:.3f}")
+    assert none < 1.5 * usual and flat < 1.5 * usual
