@@ -11,6 +11,9 @@
  * Arithmetic: inputs are widened to fp32 exactly, results are rounded once to the output's type, to nearest; sums are fp32 over at
  * most 256 rows of a thread and what its block adds to them, and fp64 beyond; products of matrices are exact and added up in
  * fp32 over at most 8192 rows, and in fp64 beyond.  The order of every sum is fixed by the sizes, so equal calls give equal bits.
+ *
+ * Operands that lie between one another are told apart exactly; at strides that differ, more than 2^22 runs of both that do so count as
+ * sharing memory.
  */
 #ifndef LIEC_ACTIVATIONS_H
 #define LIEC_ACTIVATIONS_H
@@ -94,7 +97,8 @@ liec_status liec_group_norm(const liec_images *x, const liec_param *weight, cons
  *   dweight, dbias  as in liec_layer_norm_backward: written, zeros where there is nothing to add up; stride 0 takes the sum over all
  *                workers; memory of their own, that of weight and bias not among it
  *   mean, rstd   as liec_group_norm left them
- * Where z is so near to zero that fp32 does not tell its sign, ReLU's derivative is decided in fp64.
+ * Where z is so near to zero that fp32 does not tell its sign, ReLU's derivative is decided in fp64.  SiLU's z and slope are 0 where
+ * exp(-z) is beyond fp32; results under 2^-119 may come as 0 before that.
  */
 liec_status liec_group_norm_backward(const liec_images *dy, const liec_images *x, const liec_checkpoint *saved, const float *mean,
                                      const float *rstd, const liec_param *weight, const liec_param *bias, const liec_images *dx,
@@ -108,7 +112,8 @@ typedef struct {
     int64_t worker_stride, row_stride;
 } liec_matrices;
 
-/* Bytes of scratch that liec_weight_grad needs; -1 for bad arguments.  Host only. */
+/* Bytes of scratch that liec_weight_grad needs; -1 for bad arguments.  Host only.  None where the rows are not split; otherwise the fp32 sums
+ * of each split, 4 N O (C + 1) bytes: of up to 8192 rows, or of fewer where there are few weights, then for at most 512 blocks in all. */
 int64_t liec_weight_grad_workspace(int32_t N, int64_t R, int64_t O, int64_t C);
 
 /*
@@ -120,7 +125,8 @@ int64_t liec_weight_grad_workspace(int32_t N, int64_t R, int64_t O, int64_t C);
  *   dbias        [N, O] of param_dtype, or NULL, or data = NULL; for N > 1 its stride is at least O in size
  *   1 <= N <= 65535, 0 <= R < 2^31, 1 <= O, C <= 2^24, N O C, N R O and N R C at most 2^40; no rows: zeros
  * dweight and dbias are written, not added to, and share no memory with other operands.  Products are exact: what the
- * checkpoint stands for is a bf16 number, dy one (bf16), two (fp16) or three (fp32) of them.
+ * checkpoint stands for is a bf16 number, dy one (bf16), two (fp16) or three (fp32) of them; bits of an fp32 dy under 2^-133, which values
+ * under 2^-110 can have, are left out.
  */
 liec_status liec_weight_grad(const liec_rows *dy, const liec_checkpoint *saved, const liec_matrices *dweight, const liec_param *dbias, int32_t N,
                              int64_t R, int64_t O, int64_t C, liec_dtype dtype, liec_dtype param_dtype, void *workspace,

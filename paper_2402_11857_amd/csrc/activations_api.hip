@@ -414,7 +414,7 @@ bool valid_act(int a) { return a == LIEC_ACT_NONE || a == LIEC_ACT_RELU || a == 
 
 // ---- weight gradients ------------------------------------------------------------------------------------------------
 constexpr int64_t kWgStep = 64;        // rows that a split is a multiple of
-constexpr int64_t kWgBlocks = 512;     // that a launch should have at least, where there are rows for them
+constexpr int64_t kWgBlocks = 512;     // of a launch whose rows are split: at most, but for chains of kWgChain rows, and more than half as many if there are the rows
 
 bool valid_weight(int64_t N, int64_t R, int64_t O, int64_t C) {
     if (N < 1 || N > kMaxWorkers || R < 0 || R > kMostRows || O < 1 || C < 1 || O > ((int64_t)1 << 24) || C > ((int64_t)1 << 24)) return false;

@@ -14,8 +14,8 @@
 //
 // These are the kernels for images that no block holds: two passes over them, bound by memory and, with an activation, by arithmetic
 // beside it.  16 x 8 images of 56 x 56 x 256 bf16, ReLU: forward 36 us for the sums (5.7 TB/s), 5 for the groups, 78 for y
-// (5.2 TB/s of x and y); backward from a checkpoint 63 for the sums (4.9 TB/s), 5 for what comes of them, 96 for dx (5.4
-// TB/s). 
+// (5.2 TB/s of x and y); backward from a checkpoint 65 for the sums (4.8 TB/s), 5 for what comes of them, 98 for dx (5.3
+// TB/s).
 #pragma once
 #include <type_traits>
 
@@ -490,8 +490,8 @@ __global__ __launch_bounds__(kBlock) void k_gn_apply(GnShape s, bool keep, const
 }
 
 // ---- backward ---------------------------------------------------------------------------------------------------------
-// A ReLU's dz of a row with the signs of z in fp64.  One channel after the other, picked out here, so that these few rows do not set how
-// many registers all others take.
+// A ReLU's dz of a row with the signs of z in fp64, one channel after the other.  What these few rows need stays in registers beside all
+// others: sums over a strip take 180 to 195 of them with it (two waves to a SIMD), 114 to 122 without an activation.
 template <int V, typename R, typename G>
 __device__ __forceinline__ void gn_dz_exact(float (&g)[V], const GnParams<V>& p, const R& raw, const G& grad, const GnColumns& k) {
     float f[V];

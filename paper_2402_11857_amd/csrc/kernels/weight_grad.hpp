@@ -8,7 +8,7 @@
 // widened to bf16 on the way, and read transposed, 4 rows of 16 columns by 16 lanes.
 //
 // Large products are bound by the matrix cores and what feeds them (with 256 x 256 values per block a step's products and its traffic
-// through LDS take about as long): 8 products of 4096 x 4096 x 4096 from bf16 1083 to 1112 us, 989 to 1015 TFLOP/s, where plain bf16
+// through LDS take about as long): 8 products of 4096 x 4096 x 4096 from bf16 1083 to 1122 us, 980 to 1015 TFLOP/s, where plain bf16
 // products of a library reach 930 to 1280.  On the way there: 128 x 128 values per block 2175 us; 256 x 256, a die on tiles that share
 // rows 1726; loads without edges, stores to LDS beside the products 1361; dy from memory to LDS by itself, rows placed so that
 // reads use all banks 1178; exponents as words, reads of one place and a distance 1125; x's halves in turn 1083.  Left out: operands read a
@@ -348,7 +348,7 @@ __device__ __forceinline__ v4u wg_words(const void* from, int64_t bytes) {
     return v4u{(uint32_t)at, (uint32_t)(at >> 32) & 0xffffu, (uint32_t)max((int64_t)0, min(bytes, (int64_t)0xfffffff0)), 0x00020000u};
 }
 // 16 bytes per lane from an offset in the buffer to LDS, at `to` (the same for the wave) + 16 * lane.  The compiler does not know that it is
-// under way: wg_wait waits for it.
+// under way: wg_wait waits for it.  m0 is reserved, so that no list of changed registers may name it, and nothing else here uses it.
 __device__ __forceinline__ void wg_load_to_lds(v4u buffer, uint32_t offset, uint32_t to) {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %0, 0 offen lds" : : "s"(buffer), "v"(offset), "s"(to) : "memory");
 }
@@ -356,9 +356,9 @@ __device__ __forceinline__ void wg_load_to_lds(v4u buffer, uint32_t offset, uint
 // compiler does not know of, and it waits by itself where it uses one).
 template <int LATE>
 __device__ __forceinline__ void wg_wait() {
+    static_assert(LATE == 4 || LATE <= 0, "what there is a wait for");
     if constexpr (LATE == 4) asm volatile("s_waitcnt vmcnt(4)" : : : "memory");
-    else if constexpr (LATE == 2) asm volatile("s_waitcnt vmcnt(2)" : : : "memory");
-    else if constexpr (LATE >= 0) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    else if constexpr (LATE == 0) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
@@ -508,7 +508,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void k_weight_grad_aligned(WgShape 
             }
         };
         // A step multiplies one buffer while the next is filled: dy's rows are on their way from its start (bf16) or, like x's, from
-        // the end of the step before, and x is widened and stored beside the last products.
+        // the end of the step before, and x is widened and stored beside the last products.  (dy's loads on the way to LDS are newer than x's, and
+        // the compiler, which does not count them, waits for all of them where it needs the last of x's: half way through the step.)
         auto steps_of = [&](auto with_bias) {
             if constexpr (P == 1) {
                 direct_a(r0, lds[0]);

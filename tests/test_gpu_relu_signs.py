@@ -115,4 +115,4 @@ def test_nothing_to_decide_costs_little(shape, G, kept, dtype):
     zero = torch.zeros_like(w)
     usual, none, flat = timed(x, w, b), timed(x, zero, zero), timed(torch.full_like(x, 2.0), w, zero)
     say(f"ms of 5 calls: {usual:.3f}, no weights {none:.3f}, flat images {flat:.3f}")
-    assert none < 1.5 * usual and flat < 1.5 * usual
+    assert none < 1.6 * usual and flat < 1.6 * usual
